@@ -207,10 +207,11 @@ def run(state):
         y = (h32 * r * w).to(h.dtype)
         return y if s["sum"] is None else (y, h)
     if op == "norm_q8":
-        # 1 / rms is in the scale alone; the quotient is taken in 64 bits, for values next to a border between two 8-bit numbers
+        # 1 / rms is in the scale alone.  The product with 448 is exact in 64 bits and the quotient rounded once, so a value
+        # half way between two 8-bit numbers is there exactly and no other looks like one
         p = (h32 * w).double()
         top = p.abs().amax(1)
-        q = _round_e4m3(p / top[:, None] * E4M3_MAX).float().to(torch.float8_e4m3fn)
+        q = _round_e4m3(p * E4M3_MAX / top[:, None]).float().to(torch.float8_e4m3fn)
         scale = (top * r[:, 0].double() / E4M3_MAX).float()
         return (q, scale) if s["sum"] is None else (q, scale, h)
     # the layer's normalised and hidden rows are tensors in the stream's type
@@ -264,7 +265,7 @@ def exact(case, seed):
     if op == "norm_q8":
         p = h * d["weight"]
         top = p.abs().max(1).values
-        q, scale = nearest(p / top[:, None] * E4M3_MAX), top / rms / E4M3_MAX
+        q, scale = nearest(p * E4M3_MAX / top[:, None]), top / rms / E4M3_MAX
         return (q, scale, total) if case["delta"] else (q, scale)
     hidden = function(stored(y) @ d["w1"] + d["b1"])
     return stored(hidden) @ d["w2"] + d["b2"] + h
