@@ -59,7 +59,8 @@ typedef enum {
   TOMA_ERR_UNSUPPORTED = 7, /* N_loc > 1024, head_dim not 64/128 in bf16 mode, dim > 4096 ... */
   TOMA_ERR_CUDA = 8,        /* a CUDA runtime call or launch failed */
   TOMA_ERR_TIMEOUT = 9,     /* only ever reported through *dev_status (bit 0) */
-  TOMA_ERR_SCRATCH_LIMIT = 10 /* toma_select_static: the problem needs more than TOMA_STATIC_SCRATCH_BYTES */
+  TOMA_ERR_SCRATCH_LIMIT = 10, /* toma_select_static: the problem needs more than TOMA_STATIC_SCRATCH_BYTES */
+  TOMA_ERR_ARG = 11         /* eps not positive or not finite, unknown activation, or buffers that overlap (toma_rms_norm ... toma_mlp_layer) */
 } toma_status;
 
 /* Size of the fixed scratch array built into the library for toma_select_static (16 MiB). */
@@ -215,6 +216,67 @@ TOMA_API toma_status toma_unmerge(const toma_desc* desc, const void* w, const vo
  *   multiples of 8.  bf16 runs on the tensor cores with fp32 accumulation, fp32 on FFMA. */
 TOMA_API toma_status toma_linear(int32_t m, int32_t n, int32_t k, int32_t dtype, const void* a, const void* w, void* c,
                                  uint32_t* dev_status, void* stream);
+
+/* ---- Between the blocks ----
+ * The operators a transformer block has around its modules (the layers App. C counts are made of them; the paper leaves them
+ * to the model).  Rows of activations, residuals and results may be strided: ld* is the distance from one row to the next in
+ * elements, at least the row's length, a multiple of 16 bytes for bf16 and e4m3 and of 4 elements for the norms in fp32
+ * (TOMA_ERR_SHAPE otherwise); what lies between the rows is neither read nor written.  Results may not overlap inputs or other
+ * results except where a line below says so (TOMA_ERR_ARG; columns side by side in one strided buffer do not overlap).
+ *
+ * e4m3 is the 8-bit format of 1 sign, 4 exponent and 3 mantissa bits (largest value 448, one bit pattern of NaN a sign). */
+
+typedef enum {
+  TOMA_ACT_NONE = 0,
+  TOMA_ACT_GELU = 1,      /* v Phi(v), Phi the normal distribution function */
+  TOMA_ACT_GELU_TANH = 2, /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
+  TOMA_ACT_SILU = 3       /* v / (1 + exp(-v)) */
+} toma_act;
+
+/* Root-mean-square norm with the residual's addition, row by row:
+ *   h = x + delta, rounded to dtype;  y = h / sqrt(mean(h^2) + eps) * weight, rounded to dtype.
+ *   x, y [rows][dim]; delta [rows][dim] or NULL (h = x); weight [dim] or NULL (ones); sum [rows][dim], where h goes, or NULL
+ *   (needs delta, TOMA_ERR_NULL).  dim: a multiple of 8, at most 16384 (TOMA_ERR_UNSUPPORTED).  eps > 0.
+ *   Allowed: sum = x, sum = delta, y = x or y = delta (same address and stride).
+ * The mean is held in fp32 and overflows for magnitudes above about 1e18.  No waits, so no dev_status. */
+TOMA_API toma_status toma_rms_norm(int32_t rows, int32_t dim, int32_t dtype, const void* x, int32_t ldx, const void* delta, int32_t ldd,
+                                   const void* weight, float eps, void* sum, int32_t lds, void* y, int32_t ldy, void* stream);
+
+/* The same in bf16 with y in 8 bits: q [rows][dim] e4m3 and scale [rows] fp32 with y ~ q * scale.  With p = h * weight,
+ *   q = e4m3(448 p / max|p|), to nearest, ties to even, decided without rounding in between, and
+ *   scale = max|p| / (448 sqrt(mean(h^2) + eps)).
+ * A row whose max|p| is below 2^-100 has q = 0 and scale = 0; one with an infinity or a NaN has NaN throughout, scale too.
+ * Allowed: sum = x, sum = delta.  ldq: a multiple of 16. */
+TOMA_API toma_status toma_rms_norm_q8(int32_t rows, int32_t dim, const void* x, int32_t ldx, const void* delta, int32_t ldd, const void* weight,
+                                      float eps, void* sum, int32_t lds, void* q, int32_t ldq, float* scale, void* stream);
+
+/* Projection with its epilogue: c = act(a w + bias) + residual, rounded once to dtype (sums and epilogue in fp32).
+ *   a [m][k], w [k][n] (dense), c [m][n]; bias [n] or NULL; residual [m][n] or NULL; act: a toma_act.
+ *   bf16 needs n and k multiples of 8 and runs on the tensor cores; fp32 takes any, on FFMA.
+ *   Allowed: c = residual (same address and stride). */
+TOMA_API toma_status toma_linear_act(int32_t m, int32_t n, int32_t k, int32_t dtype, const void* a, int32_t lda, const void* w, const void* bias,
+                                     int32_t act, const void* residual, int32_t ldr, void* c, int32_t ldc, uint32_t* dev_status, void* stream);
+
+/* The same with 8-bit operands: c = act((a w^T)[i][j] a_scale[i] w_scale[j] + bias) + residual.
+ *   a [m][k] and w [n][k] e4m3 (w by output column: K innermost, as toma_quantise_weight writes it), a_scale [m] and w_scale [n]
+ *   fp32; bias, residual and c bf16.  n and k multiples of 8.  Products are exact, sums and epilogue in fp32. */
+TOMA_API toma_status toma_linear_q8(int32_t m, int32_t n, int32_t k, const void* a, int32_t lda, const float* a_scale, const void* w, int32_t ldw,
+                                    const float* w_scale, const void* bias, int32_t act, const void* residual, int32_t ldr, void* c,
+                                    int32_t ldc, uint32_t* dev_status, void* stream);
+
+/* Weights for toma_linear_q8, made once: w [k][n] bf16 (dense, the layout of toma_linear) to q [n][k] e4m3 (row stride ldq) with
+ * a scale for each output column, scale [n]; rounding and special rows (columns of w) as toma_rms_norm_q8. */
+TOMA_API toma_status toma_quantise_weight(int32_t k, int32_t n, const void* w, void* q, int32_t ldq, float* scale, void* stream);
+
+/* A whole MLP layer on all rows, beside toma_mlp: with s = x + delta (rounded to dtype; delta may be NULL: s = x),
+ *   out = s + act(norm(s) w1 + b1) w2 + b2,  norm(s) = toma_rms_norm(s) with norm_weight (NULL: ones) and eps.
+ *   x, delta, out [rows][dim], dense; w1 [dim][hidden], w2 [hidden][dim]; b1 [hidden], b2 [dim], each or NULL.  norm(s) and the
+ *   hidden rows are rounded to dtype.  dim as toma_rms_norm, hidden a multiple of 8.  Allowed: out = x, out = delta.
+ *   ws: device scratch of toma_mlp_layer_workspace_bytes(), 16-byte aligned; calls that can overlap need separate scratch. */
+TOMA_API size_t toma_mlp_layer_workspace_bytes(int32_t rows, int32_t dim, int32_t hidden, int32_t dtype);
+TOMA_API toma_status toma_mlp_layer(int32_t rows, int32_t dim, int32_t hidden, int32_t dtype, const void* x, const void* delta,
+                                    const void* norm_weight, float eps, const void* w1, const void* b1, int32_t act, const void* w2,
+                                    const void* b2, void* out, void* ws, size_t ws_bytes, uint32_t* dev_status, void* stream);
 
 /* One ToMA-wrapped attention call (Algorithm 3) with pattern reuse (Sec. 4.3.2):
  * refresh idx_state / w_state when the schedule says so, then merge, attention

@@ -17,15 +17,18 @@ LIB_PATH = os.path.join(_HERE, "libtoma_b200.so")
 
 TOMA_BF16, TOMA_F32 = 0, 1
 STATUS_NAMES = ["OK", "ERR_NULL", "ERR_SHAPE", "ERR_DTYPE", "ERR_RATIO", "ERR_TAU", "ERR_WORKSPACE",
-                "ERR_UNSUPPORTED", "ERR_CUDA", "ERR_TIMEOUT", "ERR_SCRATCH_LIMIT"]
+                "ERR_UNSUPPORTED", "ERR_CUDA", "ERR_TIMEOUT", "ERR_SCRATCH_LIMIT", "ERR_ARG"]
 
 EXPORTS = ["toma_select_static", "toma_launch_counter", "toma_test_set_tuning", "toma_test_linear_form", "toma_test_wait_timeout", "toma_workspace_bytes", "toma_weights_bytes", "toma_dest_per_tile", "toma_validate", "toma_status_str",
            "toma_select", "toma_merge_weights", "toma_merge", "toma_attention_workspace_bytes", "toma_attention_plan", "toma_attention",
            "toma_unmerge", "toma_block", "toma_block_host", "toma_linear", "toma_block_proj", "toma_attention_proj_workspace_bytes",
            "toma_attention_proj", "toma_block_mlp", "toma_mlp_workspace_bytes", "toma_mlp",
+           "toma_rms_norm", "toma_rms_norm_q8", "toma_linear_act", "toma_linear_q8", "toma_quantise_weight",
+           "toma_mlp_layer_workspace_bytes", "toma_mlp_layer",
            "toma_weights_export", "toma_weights_import", "toma_unmerge_weights_export"]
 
 UNMERGE_MODES = {"transpose": 0, "shares": 1}
+ACTIVATIONS = {"none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
 
 
 class TomaDesc(Structure):
@@ -105,6 +108,21 @@ def _load() -> ctypes.CDLL:
     lib.toma_mlp.argtypes = [c_int32] * 4 + [c_void_p] * 5 + [c_size_t, c_void_p, c_void_p]
     lib.toma_linear.restype = c_int32
     lib.toma_linear.argtypes = [c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    i, p = c_int32, c_void_p
+    lib.toma_rms_norm.restype = i
+    lib.toma_rms_norm.argtypes = [i, i, i, p, i, p, i, p, c_float, p, i, p, i, p]
+    lib.toma_rms_norm_q8.restype = i
+    lib.toma_rms_norm_q8.argtypes = [i, i, p, i, p, i, p, c_float, p, i, p, i, p, p]
+    lib.toma_linear_act.restype = i
+    lib.toma_linear_act.argtypes = [i, i, i, i, p, i, p, p, i, p, i, p, i, p, p]
+    lib.toma_linear_q8.restype = i
+    lib.toma_linear_q8.argtypes = [i, i, i, p, i, p, p, i, p, p, i, p, i, p, i, p, p]
+    lib.toma_quantise_weight.restype = i
+    lib.toma_quantise_weight.argtypes = [i, i, p, p, i, p, p]
+    lib.toma_mlp_layer_workspace_bytes.restype = c_size_t
+    lib.toma_mlp_layer_workspace_bytes.argtypes = [i] * 4
+    lib.toma_mlp_layer.restype = i
+    lib.toma_mlp_layer.argtypes = [i] * 4 + [p, p, p, c_float, p, p, i, p, p, p, p, c_size_t, p, p]
     lib.toma_block_host.restype = c_int32
     lib.toma_block_host.argtypes = [P, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                     c_size_t, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
@@ -315,6 +333,153 @@ def toma_mlp_workspace_bytes(rows, dim, hidden, dtype) -> int:
 def toma_mlp(rows, dim, hidden, dtype, x, w1, w2, out, ws, dev_status=None):
     _check(lib.toma_mlp(rows, dim, hidden, _dtype_code(dtype), _ptr(x), _ptr(w1), _ptr(w2), _ptr(out), _ptr(ws),
                         ws.numel() * ws.element_size(), _ptr(dev_status), _stream()), "toma_mlp")
+
+
+# ---- between the blocks ----
+# Tensors are checked here (type, shape, device); strides, sizes and overlaps by the library.
+
+_LD_UNIT = {torch.bfloat16: 8, torch.float32: 4, torch.float8_e4m3fn: 16}
+
+
+def _rows(t, name, dtype, rows, cols, device):
+    """(data pointer, row stride) of a [rows, cols] tensor whose rows may be strided; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name}: expected {dtype} of {[rows, cols]}, got {t.dtype} of {list(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: must live on the current CUDA device")
+    ld, step = t.stride()
+    if step != 1:
+        raise ValueError(f"{name}: columns must be contiguous")
+    if rows == 1:  # the stride of a single row is no one's
+        unit = _LD_UNIT[dtype]
+        ld = (cols + unit - 1) // unit * unit
+    return t.data_ptr(), ld
+
+
+def _vec(t, name, dtype, n, device):
+    """Data pointer of a contiguous vector of n elements; None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != 1 or t.numel() != n:
+        raise ValueError(f"{name}: expected {dtype} of [{n}], got {t.dtype} of {list(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: must live on the current CUDA device")
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name}: must be contiguous")
+    return t.data_ptr()
+
+
+def _dense(t, name, dtype, rows, cols, device):
+    ptr, ld = _rows(t, name, dtype, rows, cols, device)
+    if ptr is not None and rows > 1 and ld != cols:
+        raise ValueError(f"{name}: must be contiguous")
+    return ptr
+
+
+def _matrix(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected a matrix, got {list(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must live on a CUDA device (no CPU path exists)")
+    return t.shape
+
+
+def _float_code(t, name) -> int:
+    if t.dtype == torch.bfloat16:
+        return TOMA_BF16
+    if t.dtype == torch.float32:
+        return TOMA_F32
+    raise ValueError(f"{name}: expected bfloat16 or float32, got {t.dtype}")
+
+
+def _current_device() -> int:
+    return torch.cuda.current_device() if _device is None else _device()
+
+
+def _act(act) -> int:
+    return ACTIVATIONS.get(act, -1) if isinstance(act, str) else int(act)
+
+
+def toma_rms_norm(x, weight, y, eps=1e-6, delta=None, sum_out=None):
+    """y = rms_norm(x + delta) * weight, and the sum into sum_out: [rows, dim] tensors (rows may be strided) of one type, bf16
+    or fp32.  weight [dim] or None; delta and sum_out or None.  sum_out and y may be x or delta themselves."""
+    rows, dim = _matrix(x, "x")
+    code, dt, dev = _float_code(x, "x"), x.dtype, _current_device()
+    px, ldx = _rows(x, "x", dt, rows, dim, dev)
+    pd, ldd = _rows(delta, "delta", dt, rows, dim, dev)
+    ps, lds = _rows(sum_out, "sum_out", dt, rows, dim, dev)
+    py, ldy = _rows(y, "y", dt, rows, dim, dev)
+    _check(lib.toma_rms_norm(rows, dim, code, px, ldx, pd, ldd, _vec(weight, "weight", dt, dim, dev), eps, ps, lds, py, ldy, _stream()),
+           "toma_rms_norm")
+
+
+def toma_rms_norm_q8(x, weight, q, scale, eps=1e-6, delta=None, sum_out=None):
+    """toma_rms_norm of bf16 rows with an 8-bit result: q [rows, dim] float8_e4m3fn (row stride a multiple of 16), scale [rows]
+    fp32, y ~ q * scale[:, None]."""
+    rows, dim = _matrix(x, "x")
+    dt, dev = torch.bfloat16, _current_device()
+    px, ldx = _rows(x, "x", dt, rows, dim, dev)
+    pd, ldd = _rows(delta, "delta", dt, rows, dim, dev)
+    ps, lds = _rows(sum_out, "sum_out", dt, rows, dim, dev)
+    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, rows, dim, dev)
+    _check(lib.toma_rms_norm_q8(rows, dim, px, ldx, pd, ldd, _vec(weight, "weight", dt, dim, dev), eps, ps, lds, pq, ldq,
+                                _vec(scale, "scale", torch.float32, rows, dev), _stream()), "toma_rms_norm_q8")
+
+
+def toma_linear_act(a, w, c, bias=None, act="none", residual=None, dev_status=None):
+    """c = act(a @ w + bias) + residual: a [m, k], w [k, n], c and residual [m, n], bias [n], all bf16 or all fp32; rows of a, c
+    and residual may be strided, c may be residual.  act: "none", "gelu", "gelu_tanh" or "silu"."""
+    m, k = _matrix(a, "a")
+    n = _matrix(w, "w")[1]
+    code, dt, dev = _float_code(a, "a"), a.dtype, _current_device()
+    pa, lda = _rows(a, "a", dt, m, k, dev)
+    pr, ldr = _rows(residual, "residual", dt, m, n, dev)
+    pc, ldc = _rows(c, "c", dt, m, n, dev)
+    _check(lib.toma_linear_act(m, n, k, code, pa, lda, _dense(w, "w", dt, k, n, dev), _vec(bias, "bias", dt, n, dev), _act(act), pr, ldr, pc, ldc,
+                               _ptr(dev_status), _stream()), "toma_linear_act")
+
+
+def toma_linear_q8(a, a_scale, w, w_scale, c, bias=None, act="none", residual=None, dev_status=None):
+    """c = act((a @ w.T) * a_scale[:, None] * w_scale + bias) + residual: a [m, k] and w [n, k] float8_e4m3fn (row strides
+    multiples of 16), scales fp32; c, bias and residual bf16."""
+    m, k = _matrix(a, "a")
+    n = _matrix(w, "w")[0]
+    f8, dt, dev = torch.float8_e4m3fn, torch.bfloat16, _current_device()
+    pa, lda = _rows(a, "a", f8, m, k, dev)
+    pw, ldw = _rows(w, "w", f8, n, k, dev)
+    pr, ldr = _rows(residual, "residual", dt, m, n, dev)
+    pc, ldc = _rows(c, "c", dt, m, n, dev)
+    _check(lib.toma_linear_q8(m, n, k, pa, lda, _vec(a_scale, "a_scale", torch.float32, m, dev), pw, ldw,
+                              _vec(w_scale, "w_scale", torch.float32, n, dev), _vec(bias, "bias", dt, n, dev), _act(act), pr, ldr, pc, ldc,
+                              _ptr(dev_status), _stream()), "toma_linear_q8")
+
+
+def toma_quantise_weight(w, q, scale):
+    """w [k, n] bf16 -> q [n, k] float8_e4m3fn and scale [n] fp32 for toma_linear_q8 (once per weight)."""
+    k, n = _matrix(w, "w")
+    dev = _current_device()
+    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, n, k, dev)
+    _check(lib.toma_quantise_weight(k, n, _dense(w, "w", torch.bfloat16, k, n, dev), pq, ldq, _vec(scale, "scale", torch.float32, n, dev), _stream()),
+           "toma_quantise_weight")
+
+
+def toma_mlp_layer_workspace_bytes(rows, dim, hidden, dtype) -> int:
+    return int(lib.toma_mlp_layer_workspace_bytes(rows, dim, hidden, _dtype_code(dtype)))
+
+
+def toma_mlp_layer(x, norm_weight, w1, b1, w2, b2, out, ws, act="gelu", eps=1e-6, delta=None, dev_status=None):
+    """out = s + act(rms_norm(s) * norm_weight @ w1 + b1) @ w2 + b2 with s = x + delta: x, delta and out [rows, dim] contiguous,
+    w1 [dim, hidden], w2 [hidden, dim]; norm_weight, b1, b2 and delta or None; out may be x or delta."""
+    rows, dim = _matrix(x, "x")
+    hidden = _matrix(w1, "w1")[1]
+    code, dt, dev = _float_code(x, "x"), x.dtype, _current_device()
+    _check(lib.toma_mlp_layer(rows, dim, hidden, code, _dense(x, "x", dt, rows, dim, dev), _dense(delta, "delta", dt, rows, dim, dev),
+                              _vec(norm_weight, "norm_weight", dt, dim, dev), eps, _dense(w1, "w1", dt, dim, hidden, dev),
+                              _vec(b1, "b1", dt, hidden, dev), _act(act), _dense(w2, "w2", dt, hidden, dim, dev), _vec(b2, "b2", dt, dim, dev),
+                              _dense(out, "out", dt, rows, dim, dev), _ptr(ws), ws.numel() * ws.element_size(), _ptr(dev_status), _stream()),
+           "toma_mlp_layer")
 
 
 def toma_block_host(desc, step, x_host, out_host, x_dev, out_dev, idx_state, w_state, ws, dev_status=None,

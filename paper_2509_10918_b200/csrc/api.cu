@@ -205,6 +205,7 @@ const char* toma_status_str(toma_status s) {
     case TOMA_ERR_CUDA: return "CUDA error";
     case TOMA_ERR_TIMEOUT: return "device-side wait timed out";
     case TOMA_ERR_SCRATCH_LIMIT: return "problem does not fit the built-in static scratch";
+    case TOMA_ERR_ARG: return "bad eps or activation, or buffers that overlap";
   }
   return "unknown";
 }
@@ -430,6 +431,158 @@ toma_status toma_mlp(int32_t rows, int32_t dim, int32_t hidden, int32_t dtype, c
   void* outs[1] = {out};
   cudaError_t e = do_linear(rows, hidden, dim, f32, x, w1s, hid, 1, kActGelu, dev_status, s);
   if (e == cudaSuccess) e = do_linear(rows, dim, hidden, f32, ws, w2s, outs, 1, kActNone, dev_status, s);
+  return cuda_ok(e);
+}
+
+// ---- between the blocks ----
+
+// Rows of a tensor in memory (bytes); p may be NULL.
+struct Rows {
+  const char* p;
+  size_t rows, bytes, pitch;
+};
+static Rows rows_of(const void* p, int rows, int cols, int ld, int esz) {
+  return Rows{(const char*)p, (size_t)rows, (size_t)cols * esz, (size_t)ld * esz};
+}
+static bool overlap(const Rows& a, const Rows& b) {
+  if (!a.p || !b.p) return false;
+  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p, a1 = a0 + (a.rows - 1) * a.pitch + a.bytes, b1 = b0 + (b.rows - 1) * b.pitch + b.bytes;
+  if (a0 >= b1 || b0 >= a1) return false;
+  if (a.pitch == b.pitch) {  // columns side by side in rows of one buffer
+    const size_t off = (b0 >= a0 ? b0 - a0 : a.pitch - 1 - (a0 - b0 - 1) % a.pitch) % a.pitch;
+    if (off >= a.bytes && off + b.bytes <= a.pitch) return false;
+  }
+  return true;
+}
+static bool same(const Rows& a, const Rows& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1) && a.bytes == b.bytes; }
+static bool clash(const Rows& out, const Rows& in, bool in_place) { return overlap(out, in) && !(in_place && same(out, in)); }
+static bool bad_ld(int ld, int cols, int multiple) { return ld < cols || ld % multiple; }
+
+static toma_status norm_check(const NormOp& o, int esz, int y_esz, int ld_multiple, int ldy_multiple) {
+  if (o.rows < 1 || o.dim < 8 || o.dim % 8) return TOMA_ERR_SHAPE;
+  if (o.dim > 16384) return TOMA_ERR_UNSUPPORTED;
+  if (!o.x || !o.y || (o.sum && !o.delta)) return TOMA_ERR_NULL;
+  if (bad_ld(o.ldx, o.dim, ld_multiple) || (o.delta && bad_ld(o.ldd, o.dim, ld_multiple)) || (o.sum && bad_ld(o.lds, o.dim, ld_multiple)) ||
+      bad_ld(o.ldy, o.dim, ldy_multiple))
+    return TOMA_ERR_SHAPE;
+  if (misaligned(o.x) || misaligned(o.delta) || misaligned(o.weight) || misaligned(o.sum) || misaligned(o.y) || ((uintptr_t)o.scale & 3))
+    return TOMA_ERR_SHAPE;
+  if (!(o.eps > 0.f) || !isfinite(o.eps)) return TOMA_ERR_ARG;
+  const Rows x = rows_of(o.x, o.rows, o.dim, o.ldx, esz), d = rows_of(o.delta, o.rows, o.dim, o.ldd, esz), w = rows_of(o.weight, 1, o.dim, o.dim, esz),
+             s = rows_of(o.sum, o.rows, o.dim, o.lds, esz), y = rows_of(o.y, o.rows, o.dim, o.ldy, y_esz), c = rows_of(o.scale, 1, o.rows, o.rows, 4);
+  const bool in_place = !o.scale;  // a thread writes where it has read
+  if (clash(s, x, true) || clash(s, d, true) || overlap(s, w) || clash(y, x, in_place) || clash(y, d, in_place) || overlap(y, w) || overlap(y, s) ||
+      overlap(c, x) || overlap(c, d) || overlap(c, w) || overlap(c, s) || overlap(c, y))
+    return TOMA_ERR_ARG;
+  return TOMA_OK;
+}
+
+toma_status toma_rms_norm(int32_t rows, int32_t dim, int32_t dtype, const void* x, int32_t ldx, const void* delta, int32_t ldd, const void* weight,
+                          float eps, void* sum, int32_t lds, void* y, int32_t ldy, void* stream) {
+  if (dtype != TOMA_BF16 && dtype != TOMA_F32) return TOMA_ERR_DTYPE;
+  const bool f32 = dtype == TOMA_F32;
+  const NormOp o{rows, dim, f32, x, delta, weight, sum, y, nullptr, ldx, ldd, lds, ldy, eps};
+  if (const toma_status st = norm_check(o, f32 ? 4 : 2, f32 ? 4 : 2, f32 ? 4 : 8, f32 ? 4 : 8); st != TOMA_OK) return st;
+  return cuda_ok(launch_rms_norm(o, (cudaStream_t)stream));
+}
+
+toma_status toma_rms_norm_q8(int32_t rows, int32_t dim, const void* x, int32_t ldx, const void* delta, int32_t ldd, const void* weight, float eps,
+                             void* sum, int32_t lds, void* q, int32_t ldq, float* scale, void* stream) {
+  if (!scale) return TOMA_ERR_NULL;
+  const NormOp o{rows, dim, false, x, delta, weight, sum, q, scale, ldx, ldd, lds, ldq, eps};
+  if (const toma_status st = norm_check(o, 2, 1, 8, 16); st != TOMA_OK) return st;
+  return cuda_ok(launch_rms_norm(o, (cudaStream_t)stream));
+}
+
+// Every error of a projection with its epilogue that the host can see.
+static toma_status linear_plus_check(const LinearPlusOp& o, bool f32) {
+  if (o.M < 1 || o.N < 1 || o.K < 1) return TOMA_ERR_SHAPE;
+  if (!o.a || !o.w || !o.c || (o.f8 && (!o.a_scale || !o.w_scale))) return TOMA_ERR_NULL;
+  if (misaligned(o.a) || misaligned(o.w) || misaligned(o.c) || misaligned(o.bias) || misaligned(o.residual) || misaligned(o.w_scale) ||
+      ((uintptr_t)o.a_scale & 3))
+    return TOMA_ERR_SHAPE;
+  if (!f32 && (o.N % 8 || o.K % 8)) return TOMA_ERR_SHAPE;
+  const int in = f32 ? 1 : o.f8 ? 16 : 8, out = f32 ? 1 : 8;
+  if (bad_ld(o.lda, o.K, in) || (o.f8 && bad_ld(o.ldw, o.K, 16)) || bad_ld(o.ldc, o.N, out) || (o.residual && bad_ld(o.ldr, o.N, out)))
+    return TOMA_ERR_SHAPE;
+  if (o.act < TOMA_ACT_NONE || o.act > TOMA_ACT_SILU) return TOMA_ERR_ARG;
+  const int ie = f32 ? 4 : o.f8 ? 1 : 2, oe = f32 ? 4 : 2;
+  const Rows a = rows_of(o.a, o.M, o.K, o.lda, ie), w = o.f8 ? rows_of(o.w, o.N, o.K, o.ldw, 1) : rows_of(o.w, o.K, o.N, o.N, ie),
+             c = rows_of(o.c, o.M, o.N, o.ldc, oe);
+  if (overlap(c, a) || overlap(c, w) || overlap(c, rows_of(o.bias, 1, o.N, o.N, oe)) || clash(c, rows_of(o.residual, o.M, o.N, o.ldr, oe), true) ||
+      overlap(c, rows_of(o.a_scale, 1, o.M, o.M, 4)) || overlap(c, rows_of(o.w_scale, 1, o.N, o.N, 4)))
+    return TOMA_ERR_ARG;
+  return TOMA_OK;
+}
+
+static cudaError_t do_linear_plus(const LinearPlusOp& o, bool f32, uint32_t* dev_status, cudaStream_t s) {
+  return f32 ? launch_linear_plus_simt(o, s) : launch_linear_plus_tc(o, dev_status, s);
+}
+
+toma_status toma_linear_act(int32_t m, int32_t n, int32_t k, int32_t dtype, const void* a, int32_t lda, const void* w, const void* bias, int32_t act,
+                            const void* residual, int32_t ldr, void* c, int32_t ldc, uint32_t* dev_status, void* stream) {
+  if (dtype != TOMA_BF16 && dtype != TOMA_F32) return TOMA_ERR_DTYPE;
+  const LinearPlusOp o{m, n, k, false, a, w, bias, residual, nullptr, nullptr, c, lda, n, ldr, ldc, act};
+  if (const toma_status st = linear_plus_check(o, dtype == TOMA_F32); st != TOMA_OK) return st;
+  return cuda_ok(do_linear_plus(o, dtype == TOMA_F32, dev_status, (cudaStream_t)stream));
+}
+
+toma_status toma_linear_q8(int32_t m, int32_t n, int32_t k, const void* a, int32_t lda, const float* a_scale, const void* w, int32_t ldw,
+                           const float* w_scale, const void* bias, int32_t act, const void* residual, int32_t ldr, void* c, int32_t ldc,
+                           uint32_t* dev_status, void* stream) {
+  const LinearPlusOp o{m, n, k, true, a, w, bias, residual, a_scale, w_scale, c, lda, ldw, ldr, ldc, act};
+  if (const toma_status st = linear_plus_check(o, false); st != TOMA_OK) return st;
+  return cuda_ok(do_linear_plus(o, false, dev_status, (cudaStream_t)stream));
+}
+
+toma_status toma_quantise_weight(int32_t k, int32_t n, const void* w, void* q, int32_t ldq, float* scale, void* stream) {
+  if (k < 8 || n < 8 || k % 8 || n % 8) return TOMA_ERR_SHAPE;
+  if (!w || !q || !scale) return TOMA_ERR_NULL;
+  if (misaligned(w) || misaligned(q) || misaligned(scale) || bad_ld(ldq, k, 16)) return TOMA_ERR_SHAPE;
+  const Rows wr = rows_of(w, k, n, n, 2), qr = rows_of(q, n, k, ldq, 1), sr = rows_of(scale, 1, n, n, 4);
+  if (overlap(wr, qr) || overlap(wr, sr) || overlap(qr, sr)) return TOMA_ERR_ARG;
+  return cuda_ok(launch_quantise_weight(k, n, w, q, ldq, scale, (cudaStream_t)stream));
+}
+
+size_t toma_mlp_layer_workspace_bytes(int32_t rows, int32_t dim, int32_t hidden, int32_t dtype) {
+  if ((dtype != TOMA_BF16 && dtype != TOMA_F32) || rows < 1 || dim < 1 || hidden < 1) return 0;
+  const size_t esz = dtype == TOMA_F32 ? 4 : 2;
+  return align_up((size_t)rows * dim * esz, 256) + align_up((size_t)rows * hidden * esz, 256);
+}
+
+toma_status toma_mlp_layer(int32_t rows, int32_t dim, int32_t hidden, int32_t dtype, const void* x, const void* delta, const void* norm_weight,
+                           float eps, const void* w1, const void* b1, int32_t act, const void* w2, const void* b2, void* out, void* ws,
+                           size_t ws_bytes, uint32_t* dev_status, void* stream) {
+  if (dtype != TOMA_BF16 && dtype != TOMA_F32) return TOMA_ERR_DTYPE;
+  if (rows < 1 || dim < 8 || hidden < 8 || dim % 8 || hidden % 8) return TOMA_ERR_SHAPE;
+  if (!x || !w1 || !w2 || !out) return TOMA_ERR_NULL;
+  const bool f32 = dtype == TOMA_F32;
+  const int esz = f32 ? 4 : 2;
+  if (!ws || misaligned(ws) || ws_bytes < toma_mlp_layer_workspace_bytes(rows, dim, hidden, dtype)) return TOMA_ERR_WORKSPACE;
+  char* norm = (char*)ws;
+  char* hid = norm + align_up((size_t)rows * dim * esz, 256);
+  // s goes where the result goes: the down projection reads it there as its residual
+  const NormOp n{rows, dim, f32, x, delta, norm_weight, delta ? out : nullptr, norm, nullptr, dim, dim, dim, dim, eps};
+  const LinearPlusOp up{rows, hidden, dim, false, norm, w1, b1, nullptr, nullptr, nullptr, hid, dim, hidden, 0, hidden, act};
+  const LinearPlusOp down{rows, dim, hidden, false, hid, w2, b2, delta ? out : x, nullptr, nullptr, out, hidden, dim, dim, dim, TOMA_ACT_NONE};
+  toma_status st = norm_check(n, esz, esz, f32 ? 4 : 8, f32 ? 4 : 8);
+  if (st == TOMA_OK) st = linear_plus_check(up, f32);
+  if (st == TOMA_OK) st = linear_plus_check(down, f32);
+  if (st != TOMA_OK) return st;
+  // what a later kernel reads must not be written by an earlier one, and scratch is nobody else's
+  const Rows scratch = rows_of(ws, 1, 1, 1, 1);
+  const Rows whole{scratch.p, 1, toma_mlp_layer_workspace_bytes(rows, dim, hidden, dtype), toma_mlp_layer_workspace_bytes(rows, dim, hidden, dtype)};
+  const Rows o = rows_of(out, rows, dim, dim, esz);
+  const Rows ins[] = {rows_of(x, rows, dim, dim, esz), rows_of(delta, rows, dim, dim, esz), rows_of(norm_weight, 1, dim, dim, esz),
+                      rows_of(w1, dim, hidden, hidden, esz), rows_of(b1, 1, hidden, hidden, esz), rows_of(w2, hidden, dim, dim, esz),
+                      rows_of(b2, 1, dim, dim, esz)};
+  for (int i = 0; i < 7; ++i)
+    if (overlap(whole, ins[i]) || clash(o, ins[i], i < 2)) return TOMA_ERR_ARG;
+  if (overlap(whole, o)) return TOMA_ERR_ARG;
+  cudaStream_t s = (cudaStream_t)stream;
+  cudaError_t e = launch_rms_norm(n, s);
+  if (e == cudaSuccess) e = do_linear_plus(up, f32, dev_status, s);
+  if (e == cudaSuccess) e = do_linear_plus(down, f32, dev_status, s);
   return cuda_ok(e);
 }
 

@@ -130,13 +130,38 @@ cudaError_t launch_global_idx(const Geom& g, const int32_t* idx, int32_t* gidx, 
 // Projection c = a w (a [M][K], w [K][N], c [M][N], row-major): tensor-core form for bf16 (up to three
 // weight / output pairs sharing a), FFMA form otherwise.
 // `act`: kActNone, or kActGelu to apply the exact (erf) GELU to the fp32 result before it is stored.
-constexpr int kActNone = 0, kActGelu = 1;
+constexpr int kActNone = TOMA_ACT_NONE, kActGelu = TOMA_ACT_GELU, kActGeluTanh = TOMA_ACT_GELU_TANH, kActSilu = TOMA_ACT_SILU;
 bool linear_tc_shape_ok(int M, int N, int K);
 // The tile form launch_linear_tc takes on a device of `sms` SMs that holds `pairs` clusters of two at once.
 int linear_tc_form(int M, int N, int K, int n_mats, int sms, int pairs);
 cudaError_t launch_linear_tc(int M, int N, int K, const void* a, const void* const* w, void* const* c, int n_mats, int act,
                              uint32_t* dev_status, cudaStream_t s);
 cudaError_t launch_linear_simt(int M, int N, int K, bool f32, const void* a, const void* w, void* c, int act, cudaStream_t s);
+// c = act(a w + bias) + residual, strides in elements.  f8: a [M][K] and w [N][K] in e4m3 with a_scale [M] and w_scale [N], else a and
+// w [K][N] in the type of c.  bias, residual: each or none.
+struct LinearPlusOp {
+  int M, N, K;
+  bool f8;
+  const void *a, *w, *bias, *residual;
+  const float *a_scale, *w_scale;
+  void* c;
+  int lda, ldw, ldr, ldc, act;
+};
+cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
+cudaError_t launch_linear_plus_simt(const LinearPlusOp& o, cudaStream_t s);  // fp32
+// w [K][N] bf16 -> q [N][K] e4m3 (row stride ldq) with scale [N].
+cudaError_t launch_quantise_weight(int K, int N, const void* w, void* q, int ldq, float* scale, cudaStream_t s);
+// y = rms_norm(x + delta) * weight and the sum; scale != nullptr: y in e4m3, its rows' scales.  delta, weight, sum: each or none.
+struct NormOp {
+  int rows, dim;
+  bool f32;
+  const void *x, *delta, *weight;
+  void *sum, *y;
+  float* scale;
+  int ldx, ldd, lds, ldy;
+  float eps;
+};
+cudaError_t launch_rms_norm(const NormOp& o, cudaStream_t s);
 cudaError_t launch_weights_export(const Geom& g, const void* w, float* dense, cudaStream_t s);
 cudaError_t launch_weights_import(const Geom& g, const float* dense, void* w, cudaStream_t s);
 

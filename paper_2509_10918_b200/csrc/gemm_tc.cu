@@ -9,6 +9,9 @@
 // other module ToMA wraps), stage their 32 rows in shared memory as 64-column slabs in the layout of the output tensor
 // map's box and store them with one TMA store per warp and slab: whole lines, asynchronous, instead of 16-byte stores to
 // 32 different rows per warp instruction.
+//
+// C = act(A W + bias) + residual (launch_linear_plus_tc) runs on the same kernels, with A and W in bf16 or in e4m3 (A with a
+// scale for each row, W stored [n][k] with a scale for each column): kPlus and kPlus8 below.
 #include <climits>
 
 #include "common.cuh"
@@ -23,6 +26,37 @@ namespace {
 constexpr int kKC = 64;                  // contraction elements per stage
 constexpr int kSlab = kKC * 128;         // [64 k][64 n] slab of W, 128-byte rows
 constexpr int kABytes = 128 * 128;       // [128 m][64 k] slab of A
+
+// What a kernel multiplies and what it does with the sums.  kPlain: bf16, up to three matrices, an activation.  kPlus: bf16, one
+// matrix, bias, activation and residual.  kPlus8: the same of e4m3 operands with scales.  A row of a stage is 128 bytes of either
+// type, so e4m3 takes the same slabs, boxes and cycles with twice the contraction elements; W is K-major there, [n][k] as stored.
+constexpr int kPlain = 0, kPlus = 1, kPlus8 = 2;
+template <int kKind> constexpr int kStepK = kKind == kPlus8 ? 2 * kKC : kKC;   // contraction elements per stage
+template <int kKind> constexpr int kMmaK = kKind == kPlus8 ? 32 : 16;          // ... per MMA (32 bytes)
+
+// The epilogue of kPlus and kPlus8.  bias, a_scale, w_scale: [n], [m], [n], each or none; residual: whether the second weight
+// map is the residual's (box and rows as the output's).
+struct LinearPlus {
+  const __nv_bfloat16* bias;
+  const float *a_scale, *w_scale;
+  bool residual;
+};
+
+// The maps of a stage's slab j of W, and the MMAs of a stage.
+template <int kKind>
+__device__ __forceinline__ void load_w(void* dst, const CUtensorMap* m, uint64_t* bar, int n, int k) {
+  if constexpr (kKind == kPlus8) tma_load_2d(dst, m, bar, k, n);
+  else tma_load_2d(dst, m, bar, n, k);
+}
+template <int kKind>
+__device__ __forceinline__ uint64_t w_desc(uint32_t wa, int kk) {
+  if constexpr (kKind == kPlus8) return smem_desc_sw128(wa + kk * 32, 16, 1024);
+  else return smem_desc_sw128(wa + kk * 2048, kSlab, 1024);
+}
+template <int kKind>
+__device__ __forceinline__ constexpr uint32_t idesc_of(int M, int N) {
+  return kKind == kPlus8 ? idesc_f16(kFmtE4M3, kFmtE4M3, false, false, M, N) : idesc_f16(kFmtBF16, kFmtBF16, false, true, M, N);
+}
 
 // GELU(v) = v Phi(v) = max(v, 0) - |v| Phi(-|v|) of two values, for results that are rounded to bf16.
 // Phi(-a) = erfcx(a / sqrt 2) / 2 * 2^(-a^2 log2(e) / 2), and erfcx(x) / 2 = t (c0 + c1 t + ... + c7 t^7) with
@@ -61,6 +95,20 @@ __device__ __forceinline__ void gelu2(uint32_t& v0, uint32_t& v1) {
   v0 = __float_as_uint(g0);
   v1 = __float_as_uint(g1);
 }
+// v sigmoid(z) with z = v (SiLU) or z = 2 sqrt(2 / pi) (v + 0.044715 v^3) (GELU by tanh: (1 + tanh u) / 2 = sigmoid(2 u)).  The
+// approximate exponential and reciprocal are within 2^-21 of v sigmoid(z), far below the rounding to bf16.
+__device__ __forceinline__ float by_sigmoid(float v, float z) { return v * rcp_mufu(1.f + ex2_mufu(-1.44269504f * z)); }
+__device__ __forceinline__ void activate2(uint32_t& v0, uint32_t& v1, int act) {
+  if (act == kActGelu) return gelu2(v0, v1);
+  const float x0 = __uint_as_float(v0), x1 = __uint_as_float(v1);
+  if (act == kActSilu) {
+    v0 = __float_as_uint(by_sigmoid(x0, x0));
+    v1 = __float_as_uint(by_sigmoid(x1, x1));
+  } else if (act == kActGeluTanh) {
+    v0 = __float_as_uint(by_sigmoid(x0, x0 * fmaf(0.0713548162f, x0 * x0, 1.59576912f)));
+    v1 = __float_as_uint(by_sigmoid(x1, x1 * fmaf(0.0713548162f, x1 * x1, 1.59576912f)));
+  }
+}
 
 // ------------------------------------------------------------------------------------------------
 // Persistent form: one CTA per SM walks over tiles of 128 rows x kCols columns.  The ring runs on across tiles, and two
@@ -75,9 +123,11 @@ constexpr int kEpiWarps = 8;
 struct PersistBars {
   uint64_t full[kMaxStages], empty[kMaxStages];
   uint64_t acc_full[2], acc_empty[2];
+  uint64_t res[kEpiWarps];  // an epilogue warp's slab of the residual is there
   uint32_t tmem_base;
   int abort_flag;
 };
+static_assert(sizeof(PersistBars) <= 256, "barrier block outgrew its reservation");
 
 template <int kCols>
 struct PersistCfg {
@@ -122,19 +172,121 @@ __device__ __forceinline__ void tile_out(uint32_t taddr, uint8_t* mine, int lane
   }
 }
 
-template <int kCols>
+// The same with bias and residual, and with the scales of 8-bit operands.  The slab of the residual comes into `mine` before the
+// sums are waited for, in the place that the results then take: nothing of it is left to wait for where a warp has one
+// slab of a tile.  A row of the tile is a thread's, so the columns' bias and scales are the same for the lanes of a warp (one
+// 16-byte read from L1 for all).
+template <int kKind>
+struct SlabOut {
+  uint8_t* mine;
+  uint64_t* res;      // this warp's residual barrier
+  uint32_t res_uses;  // slabs of the residual waited for
+  bool pending;       // one more is on its way
+  const CUtensorMap *tm_c, *tm_r;
+  LinearPlus p;
+  int M, N, act, lane;
+
+  __device__ __forceinline__ void fetch(int n, int m0) {  // the residual's slab at column n
+    if (!p.residual || m0 >= M) return;
+    pending = true;
+    if (lane != 0) return;
+    tma_store_wait_read();  // the slab staged before has been read
+    mbar_expect_tx(res, 4096);  // what lies past M or N comes as zeros and counts
+    tma_load_2d(mine, tm_r, res, n, m0);
+  }
+  // The sums of the tile are there; the first slab of the residual has been fetched.
+  __device__ __forceinline__ bool out(uint32_t taddr, int half, int slabs, int n0, int m0, uint32_t* dev_status, volatile int* abort_flag) {
+    const float row_scale = kKind == kPlus8 && m0 + lane < M ? p.a_scale[m0 + lane] : 1.f;
+#pragma unroll 1
+    for (int j = half; j < slabs; j += 2) {
+      if (j != half) fetch(n0 + j * 64, m0);
+      if (p.residual) {
+        if (m0 < M) {
+          if (!mbar_wait_warp(res, res_uses & 1, dev_status, abort_flag)) return false;
+          pending = false;
+          ++res_uses;
+        }
+      } else if (lane == 0) {
+        tma_store_wait_read();  // the slab staged before has been read
+      }
+      __syncwarp();
+#pragma unroll 1
+      for (int c = 0; c < 64; c += 32) {
+        const int n = n0 + j * 64 + c;
+        uint32_t r[32];
+        tmem_ld32(taddr + j * 64 + c, r);
+        tmem_wait_ld();
+        if constexpr (kKind == kPlus8) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            if (n + e >= N) break;
+            const float4 s = *reinterpret_cast<const float4*>(p.w_scale + n + e);
+            r[e] = __float_as_uint(__uint_as_float(r[e]) * (row_scale * s.x));
+            r[e + 1] = __float_as_uint(__uint_as_float(r[e + 1]) * (row_scale * s.y));
+            r[e + 2] = __float_as_uint(__uint_as_float(r[e + 2]) * (row_scale * s.z));
+            r[e + 3] = __float_as_uint(__uint_as_float(r[e + 3]) * (row_scale * s.w));
+          }
+        }
+        if (p.bias) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            if (n + e >= N) break;
+            const uint4 b = *reinterpret_cast<const uint4*>(p.bias + n + e);
+            const uint32_t bb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              r[e + 2 * u] = __float_as_uint(__uint_as_float(r[e + 2 * u]) + __uint_as_float(bb[u] << 16));
+              r[e + 2 * u + 1] = __float_as_uint(__uint_as_float(r[e + 2 * u + 1]) + __uint_as_float(bb[u] & 0xFFFF0000u));
+            }
+          }
+        }
+        if (act != kActNone) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) activate2(r[e], r[e + 1], act);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          uint4* at = reinterpret_cast<uint4*>(mine + sw128_offset(lane, (c + e) >> 3));
+          if (p.residual) {
+            const uint4 b = *at;
+            const uint32_t bb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              r[e + 2 * u] = __float_as_uint(__uint_as_float(r[e + 2 * u]) + __uint_as_float(bb[u] << 16));
+              r[e + 2 * u + 1] = __float_as_uint(__uint_as_float(r[e + 2 * u + 1]) + __uint_as_float(bb[u] & 0xFFFF0000u));
+            }
+          }
+          __align__(16) __nv_bfloat162 q[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(__uint_as_float(r[e + 2 * u]), __uint_as_float(r[e + 2 * u + 1]));
+          *at = *reinterpret_cast<const uint4*>(q);
+        }
+      }
+      fence_proxy_async();  // the staged rows are read by the TMA engine
+      __syncwarp();
+      if (lane == 0 && m0 < M) {
+        tma_store_2d(tm_c, mine, n0 + j * 64, m0);
+        tma_store_commit();
+      }
+    }
+    return true;
+  }
+};
+
+template <int kCols, int kKind>
 __global__ void __launch_bounds__((2 + kEpiWarps) * 32, 1)
 linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                          const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ CUtensorMap tm_w2,
                          const __grid_constant__ CUtensorMap tm_c0, const __grid_constant__ CUtensorMap tm_c1,
-                         const __grid_constant__ CUtensorMap tm_c2, int M, int N, int K, int n_items, int act, uint32_t* dev_status) {
+                         const __grid_constant__ CUtensorMap tm_c2, int M, int N, int K, int n_items, int act, uint32_t* dev_status,
+                         const LinearPlus plus) {
   using C = PersistCfg<kCols>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* staging = smem + C::kStages * C::kStageBytes;
   PersistBars* bar = reinterpret_cast<PersistBars*>(staging + C::kStaging);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int nk = (K + kKC - 1) / kKC;
+  const int nk = (K + kStepK<kKind> - 1) / kStepK<kKind>;
   const int mb = (M + 127) / 128, nb = (N + kCols - 1) / kCols;
   // item -> row block (fastest: CTAs that run together share W slabs), column block, matrix
   auto m_of = [&](int item) { return item % mb * 128; };
@@ -151,6 +303,8 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
       mbar_init(&bar->acc_full[a], 1);
       mbar_init(&bar->acc_empty[a], kEpiWarps);
     }
+    if constexpr (kKind != kPlain)
+      for (int e = 0; e < kEpiWarps; ++e) mbar_init(&bar->res[e], 1);
     bar->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tm_a);
@@ -178,8 +332,8 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
           if (kc >= C::kStages && !mbar_wait(&bar->empty[s], ((kc / C::kStages) - 1) & 1, dev_status, abort_flag)) { ok = false; break; }
           uint8_t* sa = smem + s * C::kStageBytes;
           mbar_expect_tx(&bar->full[s], kABytes + slabs * kSlab);
-          tma_load_2d(sa, &tm_a, &bar->full[s], k * kKC, m0);
-          for (int j = 0; j < slabs; ++j) tma_load_2d(sa + kABytes + j * kSlab, tm_w, &bar->full[s], n0 + j * 64, k * kKC);
+          tma_load_2d(sa, &tm_a, &bar->full[s], k * kStepK<kKind>, m0);
+          for (int j = 0; j < slabs; ++j) load_w<kKind>(sa + kABytes + j * kSlab, tm_w, &bar->full[s], n0 + j * 64, k * kStepK<kKind>);
         }
       }
     }
@@ -192,15 +346,16 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
         if (n >= 2 && !mbar_wait(&bar->acc_empty[a], ((n >> 1) - 1) & 1, dev_status, abort_flag)) break;
         tc_fence_after();
         const uint32_t t_acc = tmem + a * C::kAccCols;
-        const uint32_t idesc = idesc_f16(kFmtBF16, kFmtBF16, false, true, 128, slabs_at(n_of(item)) * 64);
+        const uint32_t idesc = idesc_of<kKind>(128, slabs_at(n_of(item)) * 64);
         for (int k = 0; k < nk; ++k, ++kc) {
           const int s = kc % C::kStages;
           if (!mbar_wait(&bar->full[s], (kc / C::kStages) & 1, dev_status, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t aa = smem_u32(smem + s * C::kStageBytes), wa = aa + kABytes;
-          const int ksteps = min(kKC, K - k * kKC + 15) / 16;  // 16 contraction elements per MMA (zero filled past K)
+          // (32 bytes of contraction elements per MMA, zero filled past K)
+          const int ksteps = min(kStepK<kKind>, K - k * kStepK<kKind> + kMmaK<kKind> - 1) / kMmaK<kKind>;
           for (int kk = 0; kk < ksteps; ++kk)
-            mma_ss(t_acc, smem_desc_sw128(aa + kk * 32, 16, 1024), smem_desc_sw128(wa + kk * 2048, kSlab, 1024), idesc, k > 0 || kk > 0);
+            mma_ss<kKind == kPlus8>(t_acc, smem_desc_sw128(aa + kk * 32, 16, 1024), w_desc<kKind>(wa, kk), idesc, k > 0 || kk > 0);
           mma_commit(&bar->empty[s]);
         }
         if (!ok) break;
@@ -211,18 +366,26 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     // two warps per quarter of the rows, each with every second 64-column slab
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     uint8_t* mine = staging + (warp - 2) * 4096;
+    SlabOut<kKind> plus_out{mine, &bar->res[warp - 2], 0, false, &tm_c0, &tm_w1, plus, M, N, act, lane};
     int n = 0;
     for (int item = blockIdx.x; item < n_items; item += gridDim.x, ++n) {
       const int a = n & 1, m0 = m_of(item) + quarter * 32, n0 = n_of(item), z = z_of(item), slabs = slabs_at(n0);
       const CUtensorMap* tm_c = z == 0 ? &tm_c0 : z == 1 ? &tm_c1 : &tm_c2;
+      if constexpr (kKind != kPlain) {
+        if (half < slabs) plus_out.fetch(n0 + half * 64, m0);
+      }
       // one answer per warp: the tensor-memory loads below are warp-wide operations
       if (!__all_sync(0xffffffffu, mbar_wait(&bar->acc_full[a], (n >> 1) & 1, dev_status, abort_flag))) break;
       tc_fence_after();
       const uint32_t taddr = tmem + a * C::kAccCols + ((uint32_t)(quarter * 32) << 16);
-      tile_out(taddr, mine, lane, tm_c, half, slabs, n0, m0, M, act);
+      if constexpr (kKind == kPlain) tile_out(taddr, mine, lane, tm_c, half, slabs, n0, m0, M, act);
+      else if (!plus_out.out(taddr, half, slabs, n0, m0, dev_status, abort_flag)) break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar->acc_empty[a]);
+    }
+    if constexpr (kKind != kPlain) {  // (after a wait that ran out: what was fetched still lands)
+      if (plus_out.pending) mbar_wait_warp(plus_out.res, plus_out.res_uses & 1, dev_status, abort_flag);
     }
     if (lane == 0) tma_store_wait_read();  // shared memory must outlive the engine's reads
   }
@@ -256,16 +419,19 @@ constexpr int kPairSmem = 1024 + kPairStages * kPairStageBytes + kPairStaging + 
 struct PairBars {
   uint64_t full[kPairStages], empty[kPairStages];  // (full: of the first CTA)
   uint64_t acc_full[2], acc_empty[2];
+  uint64_t res[kEpiWarps];
   uint32_t tmem_base;
   int abort_flag;
 };
 static_assert(sizeof(PairBars) <= 256, "barrier block outgrew its reservation");
 
+template <int kKind>
 __global__ void __launch_bounds__((2 + kEpiWarps) * 32, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                    const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ CUtensorMap tm_w2,
                    const __grid_constant__ CUtensorMap tm_c0, const __grid_constant__ CUtensorMap tm_c1,
-                   const __grid_constant__ CUtensorMap tm_c2, int M, int N, int K, int n_items, int act, uint32_t* dev_status) {
+                   const __grid_constant__ CUtensorMap tm_c2, int M, int N, int K, int n_items, int act, uint32_t* dev_status,
+                   const LinearPlus plus) {
   extern __shared__ uint8_t smem_raw[];
   // (the same offset in both CTAs: they are launched alike)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -273,7 +439,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
   PairBars* bar = reinterpret_cast<PairBars*>(staging + kPairStaging);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  const int nk = (K + kKC - 1) / kKC;
+  const int nk = (K + kStepK<kKind> - 1) / kStepK<kKind>;
   const int mb = (M + kPairRows - 1) / kPairRows, nb = (N + kPairCols - 1) / kPairCols;
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const int panels = (mb + kPanel - 1) / kPanel, panel = (mb + panels - 1) / panels;  // row blocks of a panel, alike but for the last
@@ -294,6 +460,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       mbar_init(&bar->acc_full[a], 1);
       mbar_init(&bar->acc_empty[a], 2 * kEpiWarps);
     }
+    if constexpr (kKind != kPlain)
+      for (int e = 0; e < kEpiWarps; ++e) mbar_init(&bar->res[e], 1);
     bar->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tm_a);
@@ -324,15 +492,18 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
           if (kc >= kPairStages && !mbar_wait(&bar->empty[s], ((kc / kPairStages) - 1) & 1, dev_status, abort_flag)) { ok = false; break; }
           uint8_t* sa = smem + s * kPairStageBytes;
           if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * kPairStageBytes);  // what lies past M or N comes as zeros and counts
-          tma_load_2d_pair(sa, &tm_a, &bar->full[s], k * kKC, m0);
-          for (int j = 0; j < 2; ++j) tma_load_2d_pair(sa + kABytes + j * kSlab, tm_w, &bar->full[s], n0 + j * 64, k * kKC);
+          tma_load_2d_pair(sa, &tm_a, &bar->full[s], k * kStepK<kKind>, m0);
+          for (int j = 0; j < 2; ++j) {
+            if constexpr (kKind == kPlus8) tma_load_2d_pair(sa + kABytes + j * kSlab, tm_w, &bar->full[s], k * kStepK<kKind>, n0 + j * 64);
+            else tma_load_2d_pair(sa + kABytes + j * kSlab, tm_w, &bar->full[s], n0 + j * 64, k * kKC);
+          }
         }
       }
     }
   } else if (warp == 1) {
     if (rank == 0) {
       if (elect_one()) {
-        constexpr uint32_t idesc = idesc_f16(kFmtBF16, kFmtBF16, false, true, kPairRows, kPairCols);
+        constexpr uint32_t idesc = idesc_of<kKind>(kPairRows, kPairCols);
         int kc = 0, n = 0;
         bool ok = true;
         for (int item = pair; ok && item < n_items; item += pairs, ++n) {
@@ -344,9 +515,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             if (!mbar_wait(&bar->full[s], (kc / kPairStages) & 1, dev_status, abort_flag)) { ok = false; break; }
             tc_fence_after();
             const uint32_t aa = smem_u32(smem + s * kPairStageBytes), wa = aa + kABytes;
-            const int ksteps = min(kKC, K - k * kKC + 15) / 16;  // 16 contraction elements per MMA (zero filled past K)
+            // (32 bytes of contraction elements per MMA, zero filled past K)
+            const int ksteps = min(kStepK<kKind>, K - k * kStepK<kKind> + kMmaK<kKind> - 1) / kMmaK<kKind>;
             for (int kk = 0; kk < ksteps; ++kk)
-              mma_ss_pair(tmem + a * 256, smem_desc_sw128(aa + kk * 32, 16, 1024), smem_desc_sw128(wa + kk * 2048, kSlab, 1024), idesc, k > 0 || kk > 0);
+              mma_ss_pair<kKind == kPlus8>(tmem + a * 256, smem_desc_sw128(aa + kk * 32, 16, 1024), w_desc<kKind>(wa, kk), idesc, k > 0 || kk > 0);
             mma_commit_pair(&bar->empty[s]);
           }
           if (ok) mma_commit_pair(&bar->acc_full[a]);
@@ -357,6 +529,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
     // two warps per quarter of the CTA's rows, each with every second 64-column slab
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     uint8_t* mine = staging + (warp - 2) * 4096;
+    SlabOut<kKind> plus_out{mine, &bar->res[warp - 2], 0, false, &tm_c0, &tm_w1, plus, M, N, act, lane};
     int n = 0;
     for (int item = pair; item < n_items; item += pairs, ++n) {
       int m0, n0, z;
@@ -364,13 +537,21 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       m0 += rank * 128 + quarter * 32;
       const int a = n & 1, slabs = (min(kPairCols, N - n0) + 63) / 64;
       const CUtensorMap* tm_c = z == 0 ? &tm_c0 : z == 1 ? &tm_c1 : &tm_c2;
+      if constexpr (kKind != kPlain) {
+        if (half < slabs) plus_out.fetch(n0 + half * 64, m0);
+      }
       // one answer per warp: the tensor-memory loads below are warp-wide operations
       if (!__all_sync(0xffffffffu, mbar_wait(&bar->acc_full[a], (n >> 1) & 1, dev_status, abort_flag))) break;
       tc_fence_after();
-      tile_out(tmem + a * 256 + ((uint32_t)(quarter * 32) << 16), mine, lane, tm_c, half, slabs, n0, m0, M, act);
+      const uint32_t taddr = tmem + a * 256 + ((uint32_t)(quarter * 32) << 16);
+      if constexpr (kKind == kPlain) tile_out(taddr, mine, lane, tm_c, half, slabs, n0, m0, M, act);
+      else if (!plus_out.out(taddr, half, slabs, n0, m0, dev_status, abort_flag)) break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_at(peer_addr(smem_u32(&bar->acc_empty[a]), 0));  // of the issuing CTA, which may be this one
+    }
+    if constexpr (kKind != kPlain) {  // (after a wait that ran out: what was fetched still lands)
+      if (plus_out.pending) mbar_wait_warp(plus_out.res, plus_out.res_uses & 1, dev_status, abort_flag);
     }
     if (lane == 0) tma_store_wait_read();  // shared memory must outlive the engine's reads
   }
@@ -383,17 +564,17 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
   cluster_sync();  // neither leaves while the other's MMAs read its shared memory or its arrivals are under way
 }
 
-template <int kCols>
+template <int kCols, int kKind>
 cudaError_t run_persistent(int M, int N, int K, int n_mats, const CUtensorMap& ta, const CUtensorMap (&tw)[3], const CUtensorMap (&tc)[3], int act,
-                           uint32_t* dev_status, cudaStream_t s) {
+                           const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
   using C = PersistCfg<kCols>;
   static std::atomic<unsigned long long> raised{0};
-  if (cudaError_t e = raise_dynamic_smem(linear_persistent_kernel<kCols>, C::kSmemBytes, raised); e != cudaSuccess) return e;
+  if (cudaError_t e = raise_dynamic_smem(linear_persistent_kernel<kCols, kKind>, C::kSmemBytes, raised); e != cudaSuccess) return e;
   const long long items = (long long)((M + 127) / 128) * ((N + kCols - 1) / kCols) * n_mats;
   if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int grid = items < sm_count() ? (int)items : sm_count();
-  return launch_dependent(linear_persistent_kernel<kCols>, dim3(grid), dim3((2 + kEpiWarps) * 32), (size_t)C::kSmemBytes, s, ta, tw[0], tw[1], tw[2],
-                          tc[0], tc[1], tc[2], M, N, K, (int)items, act, dev_status);
+  return launch_dependent(linear_persistent_kernel<kCols, kKind>, dim3(grid), dim3((2 + kEpiWarps) * 32), (size_t)C::kSmemBytes, s, ta, tw[0], tw[1],
+                          tw[2], tc[0], tc[1], tc[2], M, N, K, (int)items, act, dev_status, plus);
 }
 
 // How many pairs the device holds at once: 0 where it places no cluster of this size (asked once per device; the other forms
@@ -405,7 +586,7 @@ int pairs_at_once() {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
   if (const int k = known[dev].load(std::memory_order_relaxed)) return k - 1;
   int clusters = 0;
-  bool ok = raise_dynamic_smem(linear_pair_kernel, kPairSmem, raised) == cudaSuccess;
+  bool ok = raise_dynamic_smem(linear_pair_kernel<kPlain>, kPairSmem, raised) == cudaSuccess;
   if (ok) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2);
@@ -418,12 +599,41 @@ int pairs_at_once() {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    ok = cudaOccupancyMaxActiveClusters(&clusters, linear_pair_kernel, &cfg) == cudaSuccess;
+    ok = cudaOccupancyMaxActiveClusters(&clusters, linear_pair_kernel<kPlain>, &cfg) == cudaSuccess;
   }
   if (!ok) (void)cudaGetLastError();  // a failed query is an answer, not an error of the caller's stream
   if (!ok || clusters < 0) clusters = 0;
   known[dev].store(clusters + 1, std::memory_order_relaxed);
   return clusters;
+}
+
+// One launch in the given tile form.
+template <int kKind>
+cudaError_t run_form(int form, int at_once, int M, int N, int K, int n_mats, const CUtensorMap& ta, const CUtensorMap (&tw)[3],
+                     const CUtensorMap (&tc)[3], int act, const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
+  cudaError_t e;
+  if (form == 3) {
+    static std::atomic<unsigned long long> raised{0};
+    if ((e = raise_dynamic_smem(linear_pair_kernel<kKind>, kPairSmem, raised)) != cudaSuccess) return e;
+    const long long items = (long long)((M + kPairRows - 1) / kPairRows) * ((N + kPairCols - 1) / kPairCols) * n_mats;
+    if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
+    const int pairs = items < at_once ? (int)items : at_once;
+    e = launch_dependent_cluster(linear_pair_kernel<kKind>, dim3(2 * pairs), dim3((2 + kEpiWarps) * 32), (size_t)kPairSmem, 2, s, ta, tw[0], tw[1],
+                                 tw[2], tc[0], tc[1], tc[2], M, N, K, (int)items, act, dev_status, plus);
+  } else {
+    e = form == 4   ? run_persistent<128, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s)
+        : form == 2 ? run_persistent<192, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s)
+                    : run_persistent<256, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+  }
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// The tile form of a launch: linear_tc_form()'s, or the test's.
+int form_of(int M, int N, int K, int n_mats, int at_once) {
+  const int v = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only override
+  if (v && (v != 3 || (M > 128 && at_once > 0))) return v;
+  return linear_tc_form(M, N, K, n_mats, sm_count(), at_once);
 }
 
 }  // namespace
@@ -465,23 +675,31 @@ cudaError_t launch_linear_tc(int M, int N, int K, const void* a, const void* con
       return cudaErrorInvalidValue;
   }
   const int at_once = pairs_at_once();
-  int form = linear_tc_form(M, N, K, n_mats, sm_count(), at_once);
-  // test-only override
-  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v && (v != 3 || (M > 128 && at_once > 0))) form = v;
-  cudaError_t e;
-  if (form == 3) {
-    const long long items = (long long)((M + kPairRows - 1) / kPairRows) * ((N + kPairCols - 1) / kPairCols) * n_mats;
-    if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
-    const int pairs = items < at_once ? (int)items : at_once;
-    e = launch_dependent_cluster(linear_pair_kernel, dim3(2 * pairs), dim3((2 + kEpiWarps) * 32), (size_t)kPairSmem, 2, s, ta, tw[0], tw[1], tw[2],
-                                 tc_[0], tc_[1], tc_[2], M, N, K, (int)items, act, dev_status);
-  } else {
-    e = form == 4   ? run_persistent<128>(M, N, K, n_mats, ta, tw, tc_, act, dev_status, s)
-        : form == 2 ? run_persistent<192>(M, N, K, n_mats, ta, tw, tc_, act, dev_status, s)
-                    : run_persistent<256>(M, N, K, n_mats, ta, tw, tc_, act, dev_status, s);
-  }
-  count_launch();
-  return e != cudaSuccess ? e : cudaGetLastError();
+  return run_form<kPlain>(form_of(M, N, K, n_mats, at_once), at_once, M, N, K, n_mats, ta, tw, tc_, act, LinearPlus{}, dev_status, s);
+}
+
+// c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
+cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
+  CUtensorMap ta, tw[3], tc_[3];
+  const uint64_t adims[2] = {(uint64_t)o.K, (uint64_t)o.M}, astr[1] = {(uint64_t)o.lda * (o.f8 ? 1 : 2)};
+  const uint32_t abox[2] = {o.f8 ? 128u : 64u, 128};
+  const uint64_t wdims[2] = {(uint64_t)(o.f8 ? o.K : o.N), (uint64_t)(o.f8 ? o.N : o.K)}, wstr[1] = {(uint64_t)o.ldw * (o.f8 ? 1 : 2)};
+  const uint32_t wbox[2] = {o.f8 ? 128u : 64u, 64};
+  const uint64_t cdims[2] = {(uint64_t)o.N, (uint64_t)o.M}, cstr[1] = {(uint64_t)o.ldc * 2}, rstr[1] = {(uint64_t)o.ldr * 2};
+  const uint32_t cbox[2] = {64, 32};  // a warp's 32 rows of one 64-column slab
+  const auto encode = o.f8 ? encode_tmap_8bit : encode_tmap_16bit;
+  if (!encode(&ta, o.a, 2, adims, astr, abox) || !encode(&tw[0], o.w, 2, wdims, wstr, wbox) || !encode_tmap_16bit(&tc_[0], o.c, 2, cdims, cstr, cbox))
+    return cudaErrorInvalidValue;
+  if (!o.residual) tw[1] = tw[0];
+  else if (!encode_tmap_16bit(&tw[1], o.residual, 2, cdims, rstr, cbox)) return cudaErrorInvalidValue;
+  tw[2] = tw[0];
+  tc_[1] = tc_[2] = tc_[0];
+  const LinearPlus plus{(const __nv_bfloat16*)o.bias, o.a_scale, o.w_scale, o.residual != nullptr};
+  const int at_once = pairs_at_once();
+  // a stage of e4m3 is one of bf16 with half the contraction elements, in bytes and in cycles
+  const int form = form_of(o.M, o.N, o.f8 ? (o.K + 1) / 2 : o.K, 1, at_once);
+  return o.f8 ? run_form<kPlus8>(form, at_once, o.M, o.N, o.K, 1, ta, tw, tc_, o.act, plus, dev_status, s)
+              : run_form<kPlus>(form, at_once, o.M, o.N, o.K, 1, ta, tw, tc_, o.act, plus, dev_status, s);
 }
 
 }  // namespace toma

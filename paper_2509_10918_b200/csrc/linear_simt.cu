@@ -832,6 +832,46 @@ cudaError_t launch_linear_simt(int M, int N, int K, bool f32, const void* a, con
   return cudaGetLastError();
 }
 
+// c = act(a w + bias) + residual in fp32, rows of a, residual and c at strides of their own.  The sigmoid and the tail of the GELU
+// are taken to full precision: fp32 mode is what bf16 runs are checked against.
+struct LinearPlusF32 {
+  static constexpr bool a_k_contig = true;
+  typedef const float* APtr;
+  int M, N, K;
+  bool a_vec, b_vec, c_vec, r_vec;
+  const float *a_, *w_, *bias, *residual;
+  float* c_;
+  int lda, ldr, ldc, act;
+  __device__ __forceinline__ const float* a_ptr(int, int m) const { return a_ + (size_t)m * lda; }
+  __device__ __forceinline__ const float* b_ptr(int, int k) const { return w_ + (size_t)k * N; }
+  __device__ __forceinline__ void store4(int, int m, int n, int left, const float* v) const {
+    float f[4] = {v[0], v[1], v[2], v[3]};
+    if (bias) {
+      const float4 b = load4(bias + n, left, true);
+      f[0] += b.x, f[1] += b.y, f[2] += b.z, f[3] += b.w;
+    }
+    if (act != kActNone) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = f[e];
+        if (act == kActGelu) f[e] = 0.5f * x * erfcf(-0.70710678118654752f * x);
+        else f[e] = x / (1.f + expf(-(act == kActSilu ? x : x * fmaf(0.0713548162f, x * x, 1.59576912f))));
+      }
+    }
+    if (residual) {
+      const float4 r = load4(residual + (size_t)m * ldr + n, left, r_vec);
+      f[0] += r.x, f[1] += r.y, f[2] += r.z, f[3] += r.w;
+    }
+    put4(c_ + (size_t)m * ldc + n, left, c_vec, f);
+  }
+};
+cudaError_t launch_linear_plus_simt(const LinearPlusOp& o, cudaStream_t s) {
+  const LinearPlusF32 op{o.M, o.N, o.K, o.lda % 4 == 0, o.N % 4 == 0, o.ldc % 4 == 0, o.ldr % 4 == 0, (const float*)o.a, (const float*)o.w,
+                         (const float*)o.bias, (const float*)o.residual, (float*)o.c, o.lda, o.ldr, o.ldc, o.act};
+  run_gemm(op, 1, s);
+  return cudaGetLastError();
+}
+
 // gidx[b][p * D_loc + k] = image token of tile p's k-th pick.
 __global__ void global_idx_kernel(const int32_t* __restrict__ idx, int32_t* __restrict__ gidx, int P, int Dloc, int tiles_x,
                                   int th, int tw, int W, int total) {
