@@ -147,6 +147,9 @@ struct LinearPlusOp {
   void* c;
   int lda, ldw, ldr, ldc, act;
 };
+// The form it takes on the tensor cores: linear_tc_form()'s, 256 x 128 by pairs (5), or 128 x 128 by clusters of 2, 4, 8 that split
+// the contraction (6, 7, 8).  `steps`: of 128 bytes of a row; at2, at4, at8: clusters of the device at once.
+int linear_plus_form(int M, int N, int steps, int sms, int pairs, int at2, int at4, int at8);
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
 cudaError_t launch_linear_plus_simt(const LinearPlusOp& o, cudaStream_t s);  // fp32
 // w [K][N] bf16 -> q [N][K] e4m3 (row stride ldq) with scale [N].

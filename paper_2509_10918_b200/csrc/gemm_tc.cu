@@ -34,12 +34,12 @@ constexpr int kPlain = 0, kPlus = 1, kPlus8 = 2;
 template <int kKind> constexpr int kStepK = kKind == kPlus8 ? 2 * kKC : kKC;   // contraction elements per stage
 template <int kKind> constexpr int kMmaK = kKind == kPlus8 ? 32 : 16;          // ... per MMA (32 bytes)
 
-// The epilogue of kPlus and kPlus8.  bias, a_scale, w_scale: [n], [m], [n], each or none; residual: whether the second weight
-// map is the residual's (box and rows as the output's).
+// The epilogue of kPlus and kPlus8.  bias, a_scale, w_scale: [n], [m], [n], residual: [m][n], each or none.
 struct LinearPlus {
-  const __nv_bfloat16* bias;
+  const __nv_bfloat16 *bias, *residual;
   const float *a_scale, *w_scale;
-  bool residual;
+  __nv_bfloat16* c;
+  int ldc, ldr;
 };
 
 // The maps of a stage's slab j of W, and the MMAs of a stage.
@@ -95,18 +95,46 @@ __device__ __forceinline__ void gelu2(uint32_t& v0, uint32_t& v1) {
   v0 = __float_as_uint(g0);
   v1 = __float_as_uint(g1);
 }
-// v sigmoid(z) with z = v (SiLU) or z = 2 sqrt(2 / pi) (v + 0.044715 v^3) (GELU by tanh: (1 + tanh u) / 2 = sigmoid(2 u)).  The
-// approximate exponential and reciprocal are within 2^-21 of v sigmoid(z), far below the rounding to bf16.
-__device__ __forceinline__ float by_sigmoid(float v, float z) { return v * rcp_mufu(1.f + ex2_mufu(-1.44269504f * z)); }
-__device__ __forceinline__ void activate2(uint32_t& v0, uint32_t& v1, int act) {
-  if (act == kActGelu) return gelu2(v0, v1);
-  const float x0 = __uint_as_float(v0), x1 = __uint_as_float(v1);
-  if (act == kActSilu) {
-    v0 = __float_as_uint(by_sigmoid(x0, x0));
-    v1 = __float_as_uint(by_sigmoid(x1, x1));
+// v sigmoid(z) = v / (1 + 2^(-z log2(e))) of two values, with z = v (SiLU) or z = 2 sqrt(2 / pi) (v + 0.044715 v^3) (GELU by tanh:
+// (1 + tanh u) / 2 = sigmoid(2 u)).  The approximate exponential and reciprocal are within 2^-21 of it, far below the rounding
+// to bf16.  (A none-number in v stays one through the product with v.)
+template <int kAct>
+__device__ __forceinline__ void by_sigmoid2(uint32_t& v0, uint32_t& v1) {
+  const uint64_t v = pack2(__uint_as_float(v0), __uint_as_float(v1));
+  uint64_t z;
+  if constexpr (kAct == kActSilu) z = mul2(v, both(-1.44269504f));
+  else z = mul2(v, fma2(mul2(v, v), both(-0.102943240f), both(-2.30220819f)));
+  float z0, z1, d0, d1;
+  unpack2(z, z0, z1);
+  unpack2(add2(pack2(ex2_mufu(z0), ex2_mufu(z1)), both(1.f)), d0, d1);
+  float y0, y1;
+  unpack2(mul2(v, pack2(rcp_mufu(d0), rcp_mufu(d1))), y0, y1);
+  v0 = __float_as_uint(y0);
+  v1 = __float_as_uint(y1);
+}
+// One branch for 32 values: a branch for each pair makes a chain of their latencies (16384 x 5120 x 1280 in 8 bits 191 us so).
+__device__ __forceinline__ void activate32(uint32_t (&r)[32], int act) {
+  if (act == kActGelu) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) gelu2(r[e], r[e + 1]);
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) by_sigmoid2<kActSilu>(r[e], r[e + 1]);
   } else if (act == kActGeluTanh) {
-    v0 = __float_as_uint(by_sigmoid(x0, x0 * fmaf(0.0713548162f, x0 * x0, 1.59576912f)));
-    v1 = __float_as_uint(by_sigmoid(x1, x1 * fmaf(0.0713548162f, x1 * x1, 1.59576912f)));
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) by_sigmoid2<kActGeluTanh>(r[e], r[e + 1]);
+  }
+}
+// r += 2 e, 2 e + 1: eight bf16 of a packet.
+__device__ __forceinline__ void add_packet(uint32_t* r, const uint4& b) {
+  const uint32_t bb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    float lo, hi;
+    unpack2(add2(pack2(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1])), pack2(__uint_as_float(bb[u] << 16), __uint_as_float(bb[u] & 0xFFFF0000u))),
+            lo, hi);
+    r[2 * u] = __float_as_uint(lo);
+    r[2 * u + 1] = __float_as_uint(hi);
   }
 }
 
@@ -119,22 +147,23 @@ __device__ __forceinline__ void activate2(uint32_t& v0, uint32_t& v1, int act) {
 // ------------------------------------------------------------------------------------------------
 constexpr int kMaxStages = 6;
 constexpr int kEpiWarps = 8;
+template <int kCols, int kKind> constexpr int kOutWarps = kKind == kPlain ? kEpiWarps : kCols / 64 * 4;  // kPlus: one for each slab
 
 struct PersistBars {
   uint64_t full[kMaxStages], empty[kMaxStages];
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t res[kEpiWarps];  // an epilogue warp's slab of the residual is there
+  uint64_t res[16];  // kPlus: the residual's slab of an epilogue warp is there
   uint32_t tmem_base;
   int abort_flag;
 };
-static_assert(sizeof(PersistBars) <= 256, "barrier block outgrew its reservation");
+static_assert(sizeof(PersistBars) <= 512, "barrier block outgrew its reservation");
 
-template <int kCols>
+template <int kCols, int kKind>
 struct PersistCfg {
   static constexpr int kStageBytes = kABytes + kCols / 64 * kSlab;
-  static constexpr int kStages = kCols == 128 ? 6 : 4;
-  static constexpr int kStaging = kEpiWarps * 32 * 128;  // per epilogue warp: 32 rows of a 64-column slab
-  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 256;
+  static constexpr int kStages = kCols == 128 ? 6 : kKind != kPlain && kCols == 256 ? 3 : 4;
+  static constexpr int kStaging = kOutWarps<kCols, kKind> * 32 * 128;  // per epilogue warp: 32 rows of a 64-column slab
+  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
   static constexpr uint32_t kAccCols = kCols == 128 ? 128 : 256;
 };
 
@@ -172,115 +201,105 @@ __device__ __forceinline__ void tile_out(uint32_t taddr, uint8_t* mine, int lane
   }
 }
 
-// The same with bias and residual, and with the scales of 8-bit operands.  The slab of the residual comes into `mine` before the
-// sums are waited for, in the place that the results then take: nothing of it is left to wait for where a warp has one
-// slab of a tile.  A row of the tile is a thread's, so the columns' bias and scales are the same for the lanes of a warp (one
-// 16-byte read from L1 for all).
+// The same with bias and residual, and with the scales of 8-bit operands, a warp for each 64-column slab of a quarter: an activation
+// takes two MUFU operations and some ten instructions per value, and eight warps for 256 columns (two a scheduler) are left at
+// their latencies.  The slab of the residual comes into `mine` before the sums are waited for, in the place that the results then
+// take, so nothing of it is left to wait for.  (Packets of 32 bytes straight from and to global memory, a row a thread, were as fast
+// without a residual and 5 to 15 % slower with one.)  Bias and scales of the columns are the same for the lanes of a warp, a row
+// each: 16-byte reads out of L1 for all of them.
 template <int kKind>
 struct SlabOut {
   uint8_t* mine;
-  uint64_t* res;      // this warp's residual barrier
-  uint32_t res_uses;  // slabs of the residual waited for
-  bool pending;       // one more is on its way
+  uint64_t* res;  // this warp's residual barrier
   const CUtensorMap *tm_c, *tm_r;
   LinearPlus p;
   int M, N, act, lane;
+  uint32_t uses;  // slabs of the residual waited for
+  bool pending;   // one more is on its way
 
-  __device__ __forceinline__ void fetch(int n, int m0) {  // the residual's slab at column n
-    if (!p.residual || m0 >= M) return;
-    pending = true;
-    if (lane != 0) return;
-    tma_store_wait_read();  // the slab staged before has been read
-    mbar_expect_tx(res, 4096);  // what lies past M or N comes as zeros and counts
-    tma_load_2d(mine, tm_r, res, n, m0);
+  // The slab at column n of 32 rows from m0 on: its residual on the way into `mine`, its bias and scales into L1.
+  __device__ __forceinline__ void fetch(int n, int m0) {
+    if (lane == 0) tma_store_wait_read();  // the slab staged before has been read
+    if (p.residual && m0 < M) {
+      pending = true;
+      if (lane == 0) {
+        mbar_expect_tx(res, 4096);  // what lies past M or N comes as zeros and counts
+        tma_load_2d(mine, tm_r, res, n, m0);
+      }
+    }
+    const int c = n + 2 * lane;
+    uint32_t x;
+    if (c < N && p.bias) asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(p.bias + c));
+    if (kKind == kPlus8 && c < N) asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(p.w_scale + c));
   }
-  // The sums of the tile are there; the first slab of the residual has been fetched.
-  __device__ __forceinline__ bool out(uint32_t taddr, int half, int slabs, int n0, int m0, uint32_t* dev_status, volatile int* abort_flag) {
+  // 32 columns of the slab from c on, n in the matrix.
+  __device__ __forceinline__ void chunk(uint32_t (&r)[32], float row_scale, int n, int c) {
+    if constexpr (kKind == kPlus8) {
+      float4 s[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = n + 4 * e < N ? *reinterpret_cast<const float4*>(p.w_scale + n + 4 * e) : make_float4(0.f, 0.f, 0.f, 0.f);
+      tmem_wait_ld(r);
+      const uint64_t rs = both(row_scale);
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) {
+        const uint64_t f = mul2(rs, e % 4 == 0 ? pack2(s[e / 4].x, s[e / 4].y) : pack2(s[e / 4].z, s[e / 4].w));
+        float v0, v1;
+        unpack2(mul2(pack2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), f), v0, v1);
+        r[e] = __float_as_uint(v0);
+        r[e + 1] = __float_as_uint(v1);
+      }
+    } else {
+      tmem_wait_ld(r);
+    }
+    if (p.bias) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) add_packet(r + 8 * e, n + 8 * e < N ? *reinterpret_cast<const uint4*>(p.bias + n + 8 * e) : make_uint4(0, 0, 0, 0));
+    }
+    activate32(r, act);
+    if (p.residual) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) add_packet(r + 8 * e, *reinterpret_cast<const uint4*>(mine + sw128_offset(lane, (c >> 3) + e)));
+    }
+#pragma unroll
+    for (int e = 0; e < 32; e += 8) {
+      __align__(16) __nv_bfloat162 q[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(__uint_as_float(r[e + 2 * u]), __uint_as_float(r[e + 2 * u + 1]));
+      *reinterpret_cast<uint4*>(mine + sw128_offset(lane, (c + e) >> 3)) = *reinterpret_cast<const uint4*>(q);
+    }
+  }
+  // The sums of the slab at taddr are there and its residual has been fetched.
+  __device__ __forceinline__ bool out(uint32_t taddr, int n, int m0, uint32_t* dev_status, volatile int* abort_flag) {
     const float row_scale = kKind == kPlus8 && m0 + lane < M ? p.a_scale[m0 + lane] : 1.f;
-#pragma unroll 1
-    for (int j = half; j < slabs; j += 2) {
-      if (j != half) fetch(n0 + j * 64, m0);
-      if (p.residual) {
-        if (m0 < M) {
-          if (!mbar_wait_warp(res, res_uses & 1, dev_status, abort_flag)) return false;
-          pending = false;
-          ++res_uses;
-        }
-      } else if (lane == 0) {
-        tma_store_wait_read();  // the slab staged before has been read
-      }
-      __syncwarp();
-#pragma unroll 1
-      for (int c = 0; c < 64; c += 32) {
-        const int n = n0 + j * 64 + c;
-        uint32_t r[32];
-        tmem_ld32(taddr + j * 64 + c, r);
-        tmem_wait_ld();
-        if constexpr (kKind == kPlus8) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            if (n + e >= N) break;
-            const float4 s = *reinterpret_cast<const float4*>(p.w_scale + n + e);
-            r[e] = __float_as_uint(__uint_as_float(r[e]) * (row_scale * s.x));
-            r[e + 1] = __float_as_uint(__uint_as_float(r[e + 1]) * (row_scale * s.y));
-            r[e + 2] = __float_as_uint(__uint_as_float(r[e + 2]) * (row_scale * s.z));
-            r[e + 3] = __float_as_uint(__uint_as_float(r[e + 3]) * (row_scale * s.w));
-          }
-        }
-        if (p.bias) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            if (n + e >= N) break;
-            const uint4 b = *reinterpret_cast<const uint4*>(p.bias + n + e);
-            const uint32_t bb[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              r[e + 2 * u] = __float_as_uint(__uint_as_float(r[e + 2 * u]) + __uint_as_float(bb[u] << 16));
-              r[e + 2 * u + 1] = __float_as_uint(__uint_as_float(r[e + 2 * u + 1]) + __uint_as_float(bb[u] & 0xFFFF0000u));
-            }
-          }
-        }
-        if (act != kActNone) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) activate2(r[e], r[e + 1], act);
-        }
-#pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          uint4* at = reinterpret_cast<uint4*>(mine + sw128_offset(lane, (c + e) >> 3));
-          if (p.residual) {
-            const uint4 b = *at;
-            const uint32_t bb[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              r[e + 2 * u] = __float_as_uint(__uint_as_float(r[e + 2 * u]) + __uint_as_float(bb[u] << 16));
-              r[e + 2 * u + 1] = __float_as_uint(__uint_as_float(r[e + 2 * u + 1]) + __uint_as_float(bb[u] & 0xFFFF0000u));
-            }
-          }
-          __align__(16) __nv_bfloat162 q[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(__uint_as_float(r[e + 2 * u]), __uint_as_float(r[e + 2 * u + 1]));
-          *at = *reinterpret_cast<const uint4*>(q);
-        }
-      }
-      fence_proxy_async();  // the staged rows are read by the TMA engine
-      __syncwarp();
-      if (lane == 0 && m0 < M) {
-        tma_store_2d(tm_c, mine, n0 + j * 64, m0);
-        tma_store_commit();
-      }
+    uint32_t r[32];
+    tmem_ld32(taddr, r);
+    if (pending) {
+      if (!mbar_wait_warp(res, uses & 1, dev_status, abort_flag)) return false;
+      pending = false;
+      ++uses;
+    }
+    __syncwarp();
+    chunk(r, row_scale, n, 0);
+    tmem_ld32(taddr + 32, r);
+    chunk(r, row_scale, n + 32, 32);
+    fence_proxy_async();  // the staged rows are read by the TMA engine
+    __syncwarp();
+    if (lane == 0 && m0 < M) {
+      tma_store_2d(tm_c, mine, n, m0);
+      tma_store_commit();
     }
     return true;
   }
 };
 
 template <int kCols, int kKind>
-__global__ void __launch_bounds__((2 + kEpiWarps) * 32, 1)
+__global__ void __launch_bounds__((2 + kOutWarps<kCols, kKind>) * 32, 1)
 linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                          const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ CUtensorMap tm_w2,
                          const __grid_constant__ CUtensorMap tm_c0, const __grid_constant__ CUtensorMap tm_c1,
                          const __grid_constant__ CUtensorMap tm_c2, int M, int N, int K, int n_items, int act, uint32_t* dev_status,
                          const LinearPlus plus) {
-  using C = PersistCfg<kCols>;
+  using C = PersistCfg<kCols, kKind>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* staging = smem + C::kStages * C::kStageBytes;
@@ -301,10 +320,10 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&bar->acc_full[a], 1);
-      mbar_init(&bar->acc_empty[a], kEpiWarps);
+      mbar_init(&bar->acc_empty[a], kOutWarps<kCols, kKind>);
     }
     if constexpr (kKind != kPlain)
-      for (int e = 0; e < kEpiWarps; ++e) mbar_init(&bar->res[e], 1);
+      for (int e = 0; e < 16; ++e) mbar_init(&bar->res[e], 1);
     bar->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tm_a);
@@ -363,10 +382,10 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
       }
     }
   } else {
-    // two warps per quarter of the rows, each with every second 64-column slab
+    // two warps per quarter of the rows, each with every second 64-column slab (kPlain), or one for each slab
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     uint8_t* mine = staging + (warp - 2) * 4096;
-    SlabOut<kKind> plus_out{mine, &bar->res[warp - 2], 0, false, &tm_c0, &tm_w1, plus, M, N, act, lane};
+    SlabOut<kKind> plus_out{mine, &bar->res[warp - 2], &tm_c0, &tm_w1, plus, M, N, act, lane, 0, false};
     int n = 0;
     for (int item = blockIdx.x; item < n_items; item += gridDim.x, ++n) {
       const int a = n & 1, m0 = m_of(item) + quarter * 32, n0 = n_of(item), z = z_of(item), slabs = slabs_at(n0);
@@ -379,13 +398,13 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
       tc_fence_after();
       const uint32_t taddr = tmem + a * C::kAccCols + ((uint32_t)(quarter * 32) << 16);
       if constexpr (kKind == kPlain) tile_out(taddr, mine, lane, tm_c, half, slabs, n0, m0, M, act);
-      else if (!plus_out.out(taddr, half, slabs, n0, m0, dev_status, abort_flag)) break;
+      else if (half < slabs && !plus_out.out(taddr + half * 64, n0 + half * 64, m0, dev_status, abort_flag)) break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar->acc_empty[a]);
     }
     if constexpr (kKind != kPlain) {  // (after a wait that ran out: what was fetched still lands)
-      if (plus_out.pending) mbar_wait_warp(plus_out.res, plus_out.res_uses & 1, dev_status, abort_flag);
+      if (plus_out.pending) mbar_wait_warp(plus_out.res, plus_out.uses & 1, dev_status, abort_flag);
     }
     if (lane == 0) tma_store_wait_read();  // shared memory must outlive the engine's reads
   }
@@ -406,62 +425,71 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
 // for the last).  A k-step still takes about 650 cycles: six stages do not quite cover the way from a free slot to its loads.
 // Both CTAs' loads count on the first one's barrier; MMA completion is committed to both.
 // ------------------------------------------------------------------------------------------------
-constexpr int kPairRows = 256, kPairCols = 256, kPairStages = 6;
+constexpr int kPairRows = 256, kPairCols = 256;
 // Row blocks that are walked over together.  The 74 tiles under way then need 12 row blocks of A and six or seven column blocks
 // of W at a time, which they read in step; with all rows of A first (61 blocks and one) every k-step came out of DRAM where A is
 // larger than L2.  Panels of 4 to 16 timed on 23 shapes: 12 takes 0.95 to 1.0 of the time of all rows first (1.01 once), 8 and 16 up
 // to 1 and 2 % more than 12.  Twelve at most, all panels of a matrix alike: a last one of a few rows shares nothing (6585 x 8448 x 2112 and
 // others of 13 to 37 row blocks 3 % slower with panels of twelve and a rest).
 constexpr int kPanel = 12;
-constexpr int kPairStageBytes = kABytes + 2 * kSlab;     // a CTA's half
-constexpr int kPairStaging = kEpiWarps * 32 * 128;
-constexpr int kPairSmem = 1024 + kPairStages * kPairStageBytes + kPairStaging + 256;
+// With bias and residual there is a form of 256 x 128 besides: a CTA keeps 64 of the columns of W, half the work per tile and so
+// less of it left over where the tiles of a launch do not come out even.
+template <int kCols, int kKind>
+struct PairCfg {
+  static constexpr int kSlabs = kCols / 128;                        // of W in a CTA
+  static constexpr int kStageBytes = kABytes + kSlabs * kSlab;      // a CTA's half
+  static constexpr int kStages = kKind == kPlain ? 6 : kCols == 256 ? 5 : 8;
+  static constexpr int kStaging = kOutWarps<kCols, kKind> * 32 * 128;
+  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
+};
 struct PairBars {
-  uint64_t full[kPairStages], empty[kPairStages];  // (full: of the first CTA)
+  uint64_t full[8], empty[8];  // (full: of the first CTA)
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t res[kEpiWarps];
+  uint64_t res[16];  // kPlus: the residual's slab of an epilogue warp is there
   uint32_t tmem_base;
   int abort_flag;
 };
-static_assert(sizeof(PairBars) <= 256, "barrier block outgrew its reservation");
+static_assert(sizeof(PairBars) <= 512, "barrier block outgrew its reservation");
 
-template <int kKind>
-__global__ void __launch_bounds__((2 + kEpiWarps) * 32, 1)
+template <int kKind, int kCols>
+__global__ void __launch_bounds__((2 + kOutWarps<kCols, kKind>) * 32, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w0,
                    const __grid_constant__ CUtensorMap tm_w1, const __grid_constant__ CUtensorMap tm_w2,
                    const __grid_constant__ CUtensorMap tm_c0, const __grid_constant__ CUtensorMap tm_c1,
                    const __grid_constant__ CUtensorMap tm_c2, int M, int N, int K, int n_items, int act, uint32_t* dev_status,
                    const LinearPlus plus) {
+  using C = PairCfg<kCols, kKind>;
+  constexpr int kStages = C::kStages;
   extern __shared__ uint8_t smem_raw[];
   // (the same offset in both CTAs: they are launched alike)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* staging = smem + kPairStages * kPairStageBytes;
-  PairBars* bar = reinterpret_cast<PairBars*>(staging + kPairStaging);
+  uint8_t* staging = smem + kStages * C::kStageBytes;
+  PairBars* bar = reinterpret_cast<PairBars*>(staging + C::kStaging);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int nk = (K + kStepK<kKind> - 1) / kStepK<kKind>;
-  const int mb = (M + kPairRows - 1) / kPairRows, nb = (N + kPairCols - 1) / kPairCols;
+  const int mb = (M + kPairRows - 1) / kPairRows, nb = (N + kCols - 1) / kCols;
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const int panels = (mb + kPanel - 1) / kPanel, panel = (mb + panels - 1) / panels;  // row blocks of a panel, alike but for the last
   // item -> matrix, panel, column block, row block (fastest)
   auto place = [&](int item, int& m0, int& n0, int& z) {
     z = item / (mb * nb);
     const int in_z = item - z * mb * nb, first = in_z / (panel * nb) * panel, in_panel = in_z - first * nb, rows = min(panel, mb - first);
-    n0 = in_panel / rows * kPairCols;
+    n0 = in_panel / rows * kCols;
     m0 = (first + in_panel % rows) * kPairRows;
   };
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kPairStages; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(&bar->full[s], 1);
       mbar_init(&bar->empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&bar->acc_full[a], 1);
-      mbar_init(&bar->acc_empty[a], 2 * kEpiWarps);
+      mbar_init(&bar->acc_empty[a], 2 * kOutWarps<kCols, kKind>);
     }
     if constexpr (kKind != kPlain)
-      for (int e = 0; e < kEpiWarps; ++e) mbar_init(&bar->res[e], 1);
+      for (int e = 0; e < 16; ++e) mbar_init(&bar->res[e], 1);
     bar->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tm_a);
@@ -485,15 +513,15 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       for (int item = pair; ok && item < n_items; item += pairs) {
         int m0, n0, z;
         place(item, m0, n0, z);
-        m0 += rank * 128, n0 += rank * 128;  // this CTA's rows and columns
+        m0 += rank * 128, n0 += rank * (kCols / 2);  // this CTA's rows and columns
         const CUtensorMap* tm_w = z == 0 ? &tm_w0 : z == 1 ? &tm_w1 : &tm_w2;
         for (int k = 0; k < nk; ++k, ++kc) {
-          const int s = kc % kPairStages;
-          if (kc >= kPairStages && !mbar_wait(&bar->empty[s], ((kc / kPairStages) - 1) & 1, dev_status, abort_flag)) { ok = false; break; }
-          uint8_t* sa = smem + s * kPairStageBytes;
-          if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * kPairStageBytes);  // what lies past M or N comes as zeros and counts
+          const int s = kc % kStages;
+          if (kc >= kStages && !mbar_wait(&bar->empty[s], ((kc / kStages) - 1) & 1, dev_status, abort_flag)) { ok = false; break; }
+          uint8_t* sa = smem + s * C::kStageBytes;
+          if (rank == 0) mbar_expect_tx(&bar->full[s], 2 * C::kStageBytes);  // what lies past M or N comes as zeros and counts
           tma_load_2d_pair(sa, &tm_a, &bar->full[s], k * kStepK<kKind>, m0);
-          for (int j = 0; j < 2; ++j) {
+          for (int j = 0; j < C::kSlabs; ++j) {
             if constexpr (kKind == kPlus8) tma_load_2d_pair(sa + kABytes + j * kSlab, tm_w, &bar->full[s], k * kStepK<kKind>, n0 + j * 64);
             else tma_load_2d_pair(sa + kABytes + j * kSlab, tm_w, &bar->full[s], n0 + j * 64, k * kKC);
           }
@@ -503,7 +531,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
   } else if (warp == 1) {
     if (rank == 0) {
       if (elect_one()) {
-        constexpr uint32_t idesc = idesc_of<kKind>(kPairRows, kPairCols);
+        constexpr uint32_t idesc = idesc_of<kKind>(kPairRows, kCols);
         int kc = 0, n = 0;
         bool ok = true;
         for (int item = pair; ok && item < n_items; item += pairs, ++n) {
@@ -511,10 +539,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
           if (n >= 2 && !mbar_wait(&bar->acc_empty[a], ((n >> 1) - 1) & 1, dev_status, abort_flag)) break;
           tc_fence_after();
           for (int k = 0; k < nk; ++k, ++kc) {
-            const int s = kc % kPairStages;
-            if (!mbar_wait(&bar->full[s], (kc / kPairStages) & 1, dev_status, abort_flag)) { ok = false; break; }
+            const int s = kc % kStages;
+            if (!mbar_wait(&bar->full[s], (kc / kStages) & 1, dev_status, abort_flag)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t aa = smem_u32(smem + s * kPairStageBytes), wa = aa + kABytes;
+            const uint32_t aa = smem_u32(smem + s * C::kStageBytes), wa = aa + kABytes;
             // (32 bytes of contraction elements per MMA, zero filled past K)
             const int ksteps = min(kStepK<kKind>, K - k * kStepK<kKind> + kMmaK<kKind> - 1) / kMmaK<kKind>;
             for (int kk = 0; kk < ksteps; ++kk)
@@ -529,13 +557,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
     // two warps per quarter of the CTA's rows, each with every second 64-column slab
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     uint8_t* mine = staging + (warp - 2) * 4096;
-    SlabOut<kKind> plus_out{mine, &bar->res[warp - 2], 0, false, &tm_c0, &tm_w1, plus, M, N, act, lane};
+    SlabOut<kKind> plus_out{mine, &bar->res[warp - 2], &tm_c0, &tm_w1, plus, M, N, act, lane, 0, false};
     int n = 0;
     for (int item = pair; item < n_items; item += pairs, ++n) {
       int m0, n0, z;
       place(item, m0, n0, z);
       m0 += rank * 128 + quarter * 32;
-      const int a = n & 1, slabs = (min(kPairCols, N - n0) + 63) / 64;
+      const int a = n & 1, slabs = (min(kCols, N - n0) + 63) / 64;
       const CUtensorMap* tm_c = z == 0 ? &tm_c0 : z == 1 ? &tm_c1 : &tm_c2;
       if constexpr (kKind != kPlain) {
         if (half < slabs) plus_out.fetch(n0 + half * 64, m0);
@@ -545,13 +573,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       tc_fence_after();
       const uint32_t taddr = tmem + a * 256 + ((uint32_t)(quarter * 32) << 16);
       if constexpr (kKind == kPlain) tile_out(taddr, mine, lane, tm_c, half, slabs, n0, m0, M, act);
-      else if (!plus_out.out(taddr, half, slabs, n0, m0, dev_status, abort_flag)) break;
+      else if (half < slabs && !plus_out.out(taddr + half * 64, n0 + half * 64, m0, dev_status, abort_flag)) break;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_at(peer_addr(smem_u32(&bar->acc_empty[a]), 0));  // of the issuing CTA, which may be this one
     }
     if constexpr (kKind != kPlain) {  // (after a wait that ran out: what was fetched still lands)
-      if (plus_out.pending) mbar_wait_warp(plus_out.res, plus_out.res_uses & 1, dev_status, abort_flag);
+      if (plus_out.pending) mbar_wait_warp(plus_out.res, plus_out.uses & 1, dev_status, abort_flag);
     }
     if (lane == 0) tma_store_wait_read();  // shared memory must outlive the engine's reads
   }
@@ -567,13 +595,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
 template <int kCols, int kKind>
 cudaError_t run_persistent(int M, int N, int K, int n_mats, const CUtensorMap& ta, const CUtensorMap (&tw)[3], const CUtensorMap (&tc)[3], int act,
                            const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
-  using C = PersistCfg<kCols>;
+  using C = PersistCfg<kCols, kKind>;
   static std::atomic<unsigned long long> raised{0};
   if (cudaError_t e = raise_dynamic_smem(linear_persistent_kernel<kCols, kKind>, C::kSmemBytes, raised); e != cudaSuccess) return e;
   const long long items = (long long)((M + 127) / 128) * ((N + kCols - 1) / kCols) * n_mats;
   if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int grid = items < sm_count() ? (int)items : sm_count();
-  return launch_dependent(linear_persistent_kernel<kCols, kKind>, dim3(grid), dim3((2 + kEpiWarps) * 32), (size_t)C::kSmemBytes, s, ta, tw[0], tw[1],
+  return launch_dependent(linear_persistent_kernel<kCols, kKind>, dim3(grid), dim3((2 + kOutWarps<kCols, kKind>) * 32), (size_t)C::kSmemBytes, s, ta, tw[0], tw[1],
                           tw[2], tc[0], tc[1], tc[2], M, N, K, (int)items, act, dev_status, plus);
 }
 
@@ -586,12 +614,12 @@ int pairs_at_once() {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
   if (const int k = known[dev].load(std::memory_order_relaxed)) return k - 1;
   int clusters = 0;
-  bool ok = raise_dynamic_smem(linear_pair_kernel<kPlain>, kPairSmem, raised) == cudaSuccess;
+  bool ok = raise_dynamic_smem(linear_pair_kernel<kPlain, kPairCols>, PairCfg<kPairCols, kPlain>::kSmemBytes, raised) == cudaSuccess;
   if (ok) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2);
     cfg.blockDim = dim3((2 + kEpiWarps) * 32);
-    cfg.dynamicSmemBytes = kPairSmem;
+    cfg.dynamicSmemBytes = PairCfg<kPairCols, kPlain>::kSmemBytes;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -599,7 +627,7 @@ int pairs_at_once() {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    ok = cudaOccupancyMaxActiveClusters(&clusters, linear_pair_kernel<kPlain>, &cfg) == cudaSuccess;
+    ok = cudaOccupancyMaxActiveClusters(&clusters, linear_pair_kernel<kPlain, kPairCols>, &cfg) == cudaSuccess;
   }
   if (!ok) (void)cudaGetLastError();  // a failed query is an answer, not an error of the caller's stream
   if (!ok || clusters < 0) clusters = 0;
@@ -607,24 +635,30 @@ int pairs_at_once() {
   return clusters;
 }
 
+template <int kCols, int kKind>
+cudaError_t run_pair(int at_once, int M, int N, int K, int n_mats, const CUtensorMap& ta, const CUtensorMap (&tw)[3], const CUtensorMap (&tc)[3],
+                     int act, const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
+  using C = PairCfg<kCols, kKind>;
+  static std::atomic<unsigned long long> raised{0};
+  if (cudaError_t e = raise_dynamic_smem(linear_pair_kernel<kKind, kCols>, C::kSmemBytes, raised); e != cudaSuccess) return e;
+  const long long items = (long long)((M + kPairRows - 1) / kPairRows) * ((N + kCols - 1) / kCols) * n_mats;
+  if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
+  const int pairs = items < at_once ? (int)items : at_once;
+  return launch_dependent_cluster(linear_pair_kernel<kKind, kCols>, dim3(2 * pairs), dim3((2 + kOutWarps<kCols, kKind>) * 32), (size_t)C::kSmemBytes, 2, s, ta, tw[0],
+                                  tw[1], tw[2], tc[0], tc[1], tc[2], M, N, K, (int)items, act, dev_status, plus);
+}
+
 // One launch in the given tile form.
 template <int kKind>
 cudaError_t run_form(int form, int at_once, int M, int N, int K, int n_mats, const CUtensorMap& ta, const CUtensorMap (&tw)[3],
                      const CUtensorMap (&tc)[3], int act, const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
-  cudaError_t e;
-  if (form == 3) {
-    static std::atomic<unsigned long long> raised{0};
-    if ((e = raise_dynamic_smem(linear_pair_kernel<kKind>, kPairSmem, raised)) != cudaSuccess) return e;
-    const long long items = (long long)((M + kPairRows - 1) / kPairRows) * ((N + kPairCols - 1) / kPairCols) * n_mats;
-    if (items > INT32_MAX / 2) return cudaErrorInvalidValue;
-    const int pairs = items < at_once ? (int)items : at_once;
-    e = launch_dependent_cluster(linear_pair_kernel<kKind>, dim3(2 * pairs), dim3((2 + kEpiWarps) * 32), (size_t)kPairSmem, 2, s, ta, tw[0], tw[1],
-                                 tw[2], tc[0], tc[1], tc[2], M, N, K, (int)items, act, dev_status, plus);
-  } else {
-    e = form == 4   ? run_persistent<128, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s)
-        : form == 2 ? run_persistent<192, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s)
-                    : run_persistent<256, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
-  }
+  cudaError_t e = cudaErrorInvalidValue;
+  if (form == 4) e = run_persistent<128, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+  else if (form == 3) e = run_pair<kPairCols, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+  else if (form == 2) e = run_persistent<192, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+  else if (form == 1) e = run_persistent<256, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+  if constexpr (kKind != kPlain)
+    if (form == 5) e = run_pair<128, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -632,8 +666,224 @@ cudaError_t run_form(int form, int at_once, int M, int N, int K, int n_mats, con
 // The tile form of a launch: linear_tc_form()'s, or the test's.
 int form_of(int M, int N, int K, int n_mats, int at_once) {
   const int v = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only override
-  if (v && (v != 3 || (M > 128 && at_once > 0))) return v;
+  if (v && v <= 4 && (v != 3 || (M > 128 && at_once > 0))) return v;
   return linear_tc_form(M, N, K, n_mats, sm_count(), at_once);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Few tiles (few rows): a cluster of 2, 4 or 8 CTAs splits the contraction of one tile of 128 x 128.  Each sums up its steps in its
+// tensor memory, sends every other CTA the partial sums of the columns that one finishes (a part of 128 / S columns each, through
+// distributed shared memory, fp32), and finishes its own: the parts of all CTAs added up in the order of their ranks, then the
+// epilogue, a row a thread.  No scratch, no atomics, one launch; what is added up in which order is fixed by the shape.
+// ------------------------------------------------------------------------------------------------
+constexpr int kSplitStages = 4, kSplitStageBytes = kABytes + 2 * kSlab;
+constexpr int kSplitSmem = 1024 + kSplitStages * kSplitStageBytes + 128 * 128 * 4 + 256;
+struct SplitBars {
+  uint64_t full[kSplitStages], empty[kSplitStages], acc_full;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(SplitBars) <= 256, "barrier block outgrew its reservation");
+__device__ __forceinline__ void st_peer_v4(uint32_t addr, const uint32_t* v) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+// The epilogue of eight columns of one row, into global memory.
+template <int kKind>
+__device__ __forceinline__ void finish8(float (&v)[8], float row_scale, const LinearPlus& p, int act, const uint4& res, int n, __nv_bfloat16* c) {
+  uint32_t r[8];
+  if constexpr (kKind == kPlus8) {
+    const float4 s0 = *reinterpret_cast<const float4*>(p.w_scale + n), s1 = *reinterpret_cast<const float4*>(p.w_scale + n + 4);
+    const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= row_scale * s[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(v[e]);
+  if (p.bias) add_packet(r, *reinterpret_cast<const uint4*>(p.bias + n));
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    if (act == kActGelu) gelu2(r[e], r[e + 1]);
+    else if (act == kActSilu) by_sigmoid2<kActSilu>(r[e], r[e + 1]);
+    else if (act == kActGeluTanh) by_sigmoid2<kActGeluTanh>(r[e], r[e + 1]);
+  }
+  if (p.residual) add_packet(r, res);
+  __align__(16) __nv_bfloat162 q[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1]));
+  *reinterpret_cast<uint4*>(c) = *reinterpret_cast<const uint4*>(q);
+}
+
+template <int kKind, int S>
+__global__ void __launch_bounds__((2 + kEpiWarps) * 32, 1)
+linear_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, int M, int N, int K, int act,
+                    uint32_t* dev_status, const LinearPlus plus) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* parts = smem + kSplitStages * kSplitStageBytes;  // [other rank][column / 4][row] packets of four columns
+  SplitBars* bar = reinterpret_cast<SplitBars*>(parts + 128 * 128 * 4);
+  constexpr int kPart = 128 / S;  // columns that a CTA finishes
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_rank(), tile = blockIdx.x / S;
+  const int nk = (K + kStepK<kKind> - 1) / kStepK<kKind>, k_first = rank * nk / S, k_last = (rank + 1) * nk / S;  // (nk >= S: no CTA without a step)
+  const int mb = (M + 127) / 128, m0 = tile % mb * 128, n0 = tile / mb * 128, slabs = (min(128, N - n0) + 63) / 64;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSplitStages; ++s) {
+      mbar_init(&bar->full[s], 1);
+      mbar_init(&bar->empty[s], 1);
+    }
+    mbar_init(&bar->acc_full, 1);
+    bar->abort_flag = 0;
+    mbar_fence_init();
+    prefetch_tmap(&tm_a);
+    prefetch_tmap(&tm_w);
+  }
+  dependency_wait();
+  if (threadIdx.x == 0) release_dependents();
+  if (warp == 1) tmem_alloc(&bar->tmem_base, 128);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bar->tmem_base;
+  volatile int* abort_flag = &bar->abort_flag;
+  cluster_arrive();  // this CTA's shared memory is there: peers wait for it before they write into it
+
+  const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane, m = m0 + row;
+  const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+  constexpr int kUnits = kPart / 16;  // eights of columns that a warp finishes: the part's first or second half
+  const int c0 = rank * kPart + half * (kPart / 2);
+  uint4 res[kUnits];
+  bool ok = true;
+  if (warp == 0) {
+    if (elect_one()) {
+      for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
+        const int s = i % kSplitStages;
+        if (i >= kSplitStages && !mbar_wait(&bar->empty[s], ((i / kSplitStages) - 1) & 1, dev_status, abort_flag)) break;
+        uint8_t* sa = smem + s * kSplitStageBytes;
+        mbar_expect_tx(&bar->full[s], kABytes + slabs * kSlab);
+        tma_load_2d(sa, &tm_a, &bar->full[s], k * kStepK<kKind>, m0);
+        for (int j = 0; j < slabs; ++j) load_w<kKind>(sa + kABytes + j * kSlab, &tm_w, &bar->full[s], n0 + j * 64, k * kStepK<kKind>);
+      }
+    }
+  } else if (warp == 1) {
+    if (elect_one()) {
+      const uint32_t idesc = idesc_of<kKind>(128, slabs * 64);
+      bool all = true;
+      for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
+        const int s = i % kSplitStages;
+        if (!mbar_wait(&bar->full[s], (i / kSplitStages) & 1, dev_status, abort_flag)) { all = false; break; }
+        tc_fence_after();
+        const uint32_t aa = smem_u32(smem + s * kSplitStageBytes), wa = aa + kABytes;
+        const int ksteps = min(kStepK<kKind>, K - k * kStepK<kKind> + kMmaK<kKind> - 1) / kMmaK<kKind>;
+        for (int kk = 0; kk < ksteps; ++kk)
+          mma_ss<kKind == kPlus8>(tmem, smem_desc_sw128(aa + kk * 32, 16, 1024), w_desc<kKind>(wa, kk), idesc, k > k_first || kk > 0);
+        mma_commit(&bar->empty[s]);
+      }
+      if (all) mma_commit(&bar->acc_full);
+    }
+  } else {
+    // what the epilogue reads besides the sums, on its way while they are waited for
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int n = n0 + c0 + u * 8;
+      res[u] = plus.residual && m < M && n < N ? *reinterpret_cast<const uint4*>(plus.residual + (size_t)m * plus.ldr + n) : make_uint4(0, 0, 0, 0);
+      if (lane < 8 && n < N) {
+        uint32_t x;
+        if (plus.bias) asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(plus.bias + n));
+        if (kKind == kPlus8) asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(plus.w_scale + n + lane));
+      }
+    }
+    ok = mbar_wait_warp(&bar->acc_full, 0, dev_status, abort_flag);
+  }
+  cluster_wait();  // all peers have begun
+  if (warp >= 2 && ok && m0 + quarter * 32 < M) {
+    tc_fence_after();
+    // sixteen columns at a time to whom finishes them, the two warps of a quarter in turns
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      const int col = g * 16, to = col / kPart;
+      if ((g & 1) != half || to == rank || n0 + col >= N) continue;
+      uint32_t r[16];
+      tmem_ld16(lanes + col, r);
+      tmem_wait_ld();
+      const int slot = rank < to ? rank : rank - 1;
+      const uint32_t at = peer_addr(smem_u32(parts + ((size_t)(slot * (kPart / 4) + (col - to * kPart) / 4) * 128 + row) * 16), (uint32_t)to);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st_peer_v4(at + e * 2048, r + 4 * e);
+    }
+  }
+  cluster_arrive();
+  cluster_wait();  // the parts of all are there; nobody writes any more
+  if (warp >= 2 && ok && m0 + quarter * 32 < M) {
+    const float row_scale = kKind == kPlus8 && m < M ? plus.a_scale[m] : 1.f;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int n = n0 + c0 + u * 8, in_part = half * (kPart / 2) + u * 8;
+      if (n >= N) continue;
+      uint32_t own[8];
+      tmem_ld8(lanes + c0 + u * 8, own);
+      tmem_wait_ld();
+      float v[8] = {};
+#pragma unroll
+      for (int r = 0; r < S; ++r) {
+        if (r == rank) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(own[e]);
+        } else {
+          const uint8_t* at = parts + ((size_t)((r < rank ? r : r - 1) * (kPart / 4) + in_part / 4) * 128 + row) * 16;
+          const float4 p0 = *reinterpret_cast<const float4*>(at), p1 = *reinterpret_cast<const float4*>(at + 2048);
+          v[0] += p0.x, v[1] += p0.y, v[2] += p0.z, v[3] += p0.w, v[4] += p1.x, v[5] += p1.y, v[6] += p1.z, v[7] += p1.w;
+        }
+      }
+      if (m < M) finish8<kKind>(v, row_scale, plus, act, res[u], n, plus.c + (size_t)m * plus.ldc + n);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 128);
+  }
+}
+
+// How many clusters of S the device holds at once (asked once per device; 0: none).
+template <int kKind, int S>
+int splits_at_once() {
+  static std::atomic<unsigned long long> raised{0};
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  if (const int k = known[dev].load(std::memory_order_relaxed)) return k - 1;
+  int clusters = 0;
+  bool ok = raise_dynamic_smem(linear_split_kernel<kKind, S>, kSplitSmem, raised) == cudaSuccess;
+  if (ok) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(S);
+    cfg.blockDim = dim3((2 + kEpiWarps) * 32);
+    cfg.dynamicSmemBytes = kSplitSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = S;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ok = cudaOccupancyMaxActiveClusters(&clusters, linear_split_kernel<kKind, S>, &cfg) == cudaSuccess;
+  }
+  if (!ok) (void)cudaGetLastError();
+  if (!ok || clusters < 0) clusters = 0;
+  known[dev].store(clusters + 1, std::memory_order_relaxed);
+  return clusters;
+}
+template <int kKind, int S>
+cudaError_t run_split(int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tw, int act, const LinearPlus& plus,
+                      uint32_t* dev_status, cudaStream_t s) {
+  const long long ctas = (long long)((M + 127) / 128) * ((N + 127) / 128) * S;
+  if (ctas > INT32_MAX) return cudaErrorInvalidValue;
+  const cudaError_t e = launch_dependent_cluster(linear_split_kernel<kKind, S>, dim3((unsigned)ctas), dim3((2 + kEpiWarps) * 32), (size_t)kSplitSmem, S, s,
+                                                 ta, tw, M, N, K, act, dev_status, plus);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
@@ -678,28 +928,45 @@ cudaError_t launch_linear_tc(int M, int N, int K, const void* a, const void* con
   return run_form<kPlain>(form_of(M, N, K, n_mats, at_once), at_once, M, N, K, n_mats, ta, tw, tc_, act, LinearPlus{}, dev_status, s);
 }
 
+namespace {
+template <int kKind>
+cudaError_t run_plus(const LinearPlusOp& o, const CUtensorMap& ta, const CUtensorMap& tw, const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
+  const int at_once = pairs_at_once(), steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
+  const int at2 = splits_at_once<kKind, 2>(), at4 = splits_at_once<kKind, 4>(), at8 = splits_at_once<kKind, 8>();
+  int form = linear_plus_form(o.M, o.N, steps, sm_count(), at_once, at2, at4, at8);
+  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed)) {  // test-only override
+    const bool pair = v == 3 || v == 5, split = v >= 6 && v <= 8;
+    if (pair ? o.M > 128 && at_once > 0 : !split || (steps >= 1 << (v - 5) && (v == 6 ? at2 : v == 7 ? at4 : at8) > 0)) form = v;
+  }
+  if (form == 6) return run_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+  if (form == 7) return run_split<kKind, 4>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+  if (form == 8) return run_split<kKind, 8>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+  CUtensorMap tc, tr = tw;
+  const uint64_t cdims[2] = {(uint64_t)o.N, (uint64_t)o.M}, cstr[1] = {(uint64_t)o.ldc * 2}, rstr[1] = {(uint64_t)o.ldr * 2};
+  const uint32_t cbox[2] = {64, 32};  // a warp's 32 rows of one 64-column slab
+  if (!encode_tmap_16bit(&tc, o.c, 2, cdims, cstr, cbox) || (o.residual && !encode_tmap_16bit(&tr, o.residual, 2, cdims, rstr, cbox)))
+    return cudaErrorInvalidValue;
+  const CUtensorMap tws[3] = {tw, tr, tw}, tcs[3] = {tc, tc, tc};
+  return run_form<kKind>(form, at_once, o.M, o.N, o.K, 1, ta, tws, tcs, o.act, plus, dev_status, s);
+}
+}  // namespace
+
+// The same with bias and residual, by stages (64 contraction elements of bf16, 128 of e4m3).
+int linear_plus_form(int M, int N, int steps, int sms, int pairs, int at2, int at4, int at8) {
+  return linear_tc_form(M, N, steps * kKC, 1, sms, pairs);
+}
+
 // c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
-  CUtensorMap ta, tw[3], tc_[3];
+  CUtensorMap ta, tw;
   const uint64_t adims[2] = {(uint64_t)o.K, (uint64_t)o.M}, astr[1] = {(uint64_t)o.lda * (o.f8 ? 1 : 2)};
   const uint32_t abox[2] = {o.f8 ? 128u : 64u, 128};
   const uint64_t wdims[2] = {(uint64_t)(o.f8 ? o.K : o.N), (uint64_t)(o.f8 ? o.N : o.K)}, wstr[1] = {(uint64_t)o.ldw * (o.f8 ? 1 : 2)};
   const uint32_t wbox[2] = {o.f8 ? 128u : 64u, 64};
-  const uint64_t cdims[2] = {(uint64_t)o.N, (uint64_t)o.M}, cstr[1] = {(uint64_t)o.ldc * 2}, rstr[1] = {(uint64_t)o.ldr * 2};
-  const uint32_t cbox[2] = {64, 32};  // a warp's 32 rows of one 64-column slab
   const auto encode = o.f8 ? encode_tmap_8bit : encode_tmap_16bit;
-  if (!encode(&ta, o.a, 2, adims, astr, abox) || !encode(&tw[0], o.w, 2, wdims, wstr, wbox) || !encode_tmap_16bit(&tc_[0], o.c, 2, cdims, cstr, cbox))
-    return cudaErrorInvalidValue;
-  if (!o.residual) tw[1] = tw[0];
-  else if (!encode_tmap_16bit(&tw[1], o.residual, 2, cdims, rstr, cbox)) return cudaErrorInvalidValue;
-  tw[2] = tw[0];
-  tc_[1] = tc_[2] = tc_[0];
-  const LinearPlus plus{(const __nv_bfloat16*)o.bias, o.a_scale, o.w_scale, o.residual != nullptr};
-  const int at_once = pairs_at_once();
-  // a stage of e4m3 is one of bf16 with half the contraction elements, in bytes and in cycles
-  const int form = form_of(o.M, o.N, o.f8 ? (o.K + 1) / 2 : o.K, 1, at_once);
-  return o.f8 ? run_form<kPlus8>(form, at_once, o.M, o.N, o.K, 1, ta, tw, tc_, o.act, plus, dev_status, s)
-              : run_form<kPlus>(form, at_once, o.M, o.N, o.K, 1, ta, tw, tc_, o.act, plus, dev_status, s);
+  if (!encode(&ta, o.a, 2, adims, astr, abox) || !encode(&tw, o.w, 2, wdims, wstr, wbox)) return cudaErrorInvalidValue;
+  const LinearPlus plus{(const __nv_bfloat16*)o.bias, (const __nv_bfloat16*)o.residual, o.a_scale, o.w_scale, (__nv_bfloat16*)o.c, o.ldc, o.ldr};
+  return o.f8 ? run_plus<kPlus8>(o, ta, tw, plus, dev_status, s) : run_plus<kPlus>(o, ta, tw, plus, dev_status, s);
 }
 
 }  // namespace toma
