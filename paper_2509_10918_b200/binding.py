@@ -341,20 +341,26 @@ def toma_mlp(rows, dim, hidden, dtype, x, w1, w2, out, ws, dev_status=None):
 _LD_UNIT = {torch.bfloat16: 8, torch.float32: 4, torch.float8_e4m3fn: 16}
 
 
-def _rows(t, name, dtype, rows, cols, device):
+def _refuse(t, name, dtype, shape, device):
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected {dtype} of {list(shape)}, got {t.dtype} of {list(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: must live on the current CUDA device")
+    raise ValueError(f"{name}: must be contiguous" if len(shape) == 1 else f"{name}: columns must be contiguous")
+
+
+def _rows(t, name, dtype, shape, device):
     """(data pointer, row stride) of a [rows, cols] tensor whose rows may be strided; (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.dtype != dtype or tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{name}: expected {dtype} of {[rows, cols]}, got {t.dtype} of {list(t.shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: must live on the current CUDA device")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _refuse(t, name, dtype, shape, device)
     ld, step = t.stride()
     if step != 1:
-        raise ValueError(f"{name}: columns must be contiguous")
-    if rows == 1:  # the stride of a single row is no one's
+        _refuse(t, name, dtype, shape, device)
+    if shape[0] == 1:  # the stride of a single row is no one's
         unit = _LD_UNIT[dtype]
-        ld = (cols + unit - 1) // unit * unit
+        ld = (shape[1] + unit - 1) // unit * unit
     return t.data_ptr(), ld
 
 
@@ -362,20 +368,17 @@ def _vec(t, name, dtype, n, device):
     """Data pointer of a contiguous vector of n elements; None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != 1 or t.numel() != n:
-        raise ValueError(f"{name}: expected {dtype} of [{n}], got {t.dtype} of {list(t.shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: must live on the current CUDA device")
-    if n > 1 and t.stride(0) != 1:
-        raise ValueError(f"{name}: must be contiguous")
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, name, dtype, (n,), device)
     return t.data_ptr()
 
 
-def _dense(t, name, dtype, rows, cols, device):
-    ptr, ld = _rows(t, name, dtype, rows, cols, device)
-    if ptr is not None and rows > 1 and ld != cols:
-        raise ValueError(f"{name}: must be contiguous")
-    return ptr
+def _dense(t, name, dtype, shape, device):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, name, dtype, shape, device)
+    return t.data_ptr()
 
 
 def _matrix(t, name):
@@ -405,12 +408,12 @@ def _act(act) -> int:
 def toma_rms_norm(x, weight, y, eps=1e-6, delta=None, sum_out=None):
     """y = rms_norm(x + delta) * weight, and the sum into sum_out: [rows, dim] tensors (rows may be strided) of one type, bf16
     or fp32.  weight [dim] or None; delta and sum_out or None.  sum_out and y may be x or delta themselves."""
-    rows, dim = _matrix(x, "x")
+    shape = rows, dim = _matrix(x, "x")
     code, dt, dev = _float_code(x, "x"), x.dtype, _current_device()
-    px, ldx = _rows(x, "x", dt, rows, dim, dev)
-    pd, ldd = _rows(delta, "delta", dt, rows, dim, dev)
-    ps, lds = _rows(sum_out, "sum_out", dt, rows, dim, dev)
-    py, ldy = _rows(y, "y", dt, rows, dim, dev)
+    px, ldx = _rows(x, "x", dt, shape, dev)
+    pd, ldd = _rows(delta, "delta", dt, shape, dev)
+    ps, lds = _rows(sum_out, "sum_out", dt, shape, dev)
+    py, ldy = _rows(y, "y", dt, shape, dev)
     _check(lib.toma_rms_norm(rows, dim, code, px, ldx, pd, ldd, _vec(weight, "weight", dt, dim, dev), eps, ps, lds, py, ldy, _stream()),
            "toma_rms_norm")
 
@@ -418,12 +421,12 @@ def toma_rms_norm(x, weight, y, eps=1e-6, delta=None, sum_out=None):
 def toma_rms_norm_q8(x, weight, q, scale, eps=1e-6, delta=None, sum_out=None):
     """toma_rms_norm of bf16 rows with an 8-bit result: q [rows, dim] float8_e4m3fn (row stride a multiple of 16), scale [rows]
     fp32, y ~ q * scale[:, None]."""
-    rows, dim = _matrix(x, "x")
+    shape = rows, dim = _matrix(x, "x")
     dt, dev = torch.bfloat16, _current_device()
-    px, ldx = _rows(x, "x", dt, rows, dim, dev)
-    pd, ldd = _rows(delta, "delta", dt, rows, dim, dev)
-    ps, lds = _rows(sum_out, "sum_out", dt, rows, dim, dev)
-    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, rows, dim, dev)
+    px, ldx = _rows(x, "x", dt, shape, dev)
+    pd, ldd = _rows(delta, "delta", dt, shape, dev)
+    ps, lds = _rows(sum_out, "sum_out", dt, shape, dev)
+    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, shape, dev)
     _check(lib.toma_rms_norm_q8(rows, dim, px, ldx, pd, ldd, _vec(weight, "weight", dt, dim, dev), eps, ps, lds, pq, ldq,
                                 _vec(scale, "scale", torch.float32, rows, dev), _stream()), "toma_rms_norm_q8")
 
@@ -434,10 +437,10 @@ def toma_linear_act(a, w, c, bias=None, act="none", residual=None, dev_status=No
     m, k = _matrix(a, "a")
     n = _matrix(w, "w")[1]
     code, dt, dev = _float_code(a, "a"), a.dtype, _current_device()
-    pa, lda = _rows(a, "a", dt, m, k, dev)
-    pr, ldr = _rows(residual, "residual", dt, m, n, dev)
-    pc, ldc = _rows(c, "c", dt, m, n, dev)
-    _check(lib.toma_linear_act(m, n, k, code, pa, lda, _dense(w, "w", dt, k, n, dev), _vec(bias, "bias", dt, n, dev), _act(act), pr, ldr, pc, ldc,
+    pa, lda = _rows(a, "a", dt, (m, k), dev)
+    pr, ldr = _rows(residual, "residual", dt, (m, n), dev)
+    pc, ldc = _rows(c, "c", dt, (m, n), dev)
+    _check(lib.toma_linear_act(m, n, k, code, pa, lda, _dense(w, "w", dt, (k, n), dev), _vec(bias, "bias", dt, n, dev), _act(act), pr, ldr, pc, ldc,
                                _ptr(dev_status), _stream()), "toma_linear_act")
 
 
@@ -447,10 +450,10 @@ def toma_linear_q8(a, a_scale, w, w_scale, c, bias=None, act="none", residual=No
     m, k = _matrix(a, "a")
     n = _matrix(w, "w")[0]
     f8, dt, dev = torch.float8_e4m3fn, torch.bfloat16, _current_device()
-    pa, lda = _rows(a, "a", f8, m, k, dev)
-    pw, ldw = _rows(w, "w", f8, n, k, dev)
-    pr, ldr = _rows(residual, "residual", dt, m, n, dev)
-    pc, ldc = _rows(c, "c", dt, m, n, dev)
+    pa, lda = _rows(a, "a", f8, (m, k), dev)
+    pw, ldw = _rows(w, "w", f8, (n, k), dev)
+    pr, ldr = _rows(residual, "residual", dt, (m, n), dev)
+    pc, ldc = _rows(c, "c", dt, (m, n), dev)
     _check(lib.toma_linear_q8(m, n, k, pa, lda, _vec(a_scale, "a_scale", torch.float32, m, dev), pw, ldw,
                               _vec(w_scale, "w_scale", torch.float32, n, dev), _vec(bias, "bias", dt, n, dev), _act(act), pr, ldr, pc, ldc,
                               _ptr(dev_status), _stream()), "toma_linear_q8")
@@ -460,8 +463,8 @@ def toma_quantise_weight(w, q, scale):
     """w [k, n] bf16 -> q [n, k] float8_e4m3fn and scale [n] fp32 for toma_linear_q8 (once per weight)."""
     k, n = _matrix(w, "w")
     dev = _current_device()
-    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, n, k, dev)
-    _check(lib.toma_quantise_weight(k, n, _dense(w, "w", torch.bfloat16, k, n, dev), pq, ldq, _vec(scale, "scale", torch.float32, n, dev), _stream()),
+    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, (n, k), dev)
+    _check(lib.toma_quantise_weight(k, n, _dense(w, "w", torch.bfloat16, (k, n), dev), pq, ldq, _vec(scale, "scale", torch.float32, n, dev), _stream()),
            "toma_quantise_weight")
 
 
@@ -475,10 +478,10 @@ def toma_mlp_layer(x, norm_weight, w1, b1, w2, b2, out, ws, act="gelu", eps=1e-6
     rows, dim = _matrix(x, "x")
     hidden = _matrix(w1, "w1")[1]
     code, dt, dev = _float_code(x, "x"), x.dtype, _current_device()
-    _check(lib.toma_mlp_layer(rows, dim, hidden, code, _dense(x, "x", dt, rows, dim, dev), _dense(delta, "delta", dt, rows, dim, dev),
-                              _vec(norm_weight, "norm_weight", dt, dim, dev), eps, _dense(w1, "w1", dt, dim, hidden, dev),
-                              _vec(b1, "b1", dt, hidden, dev), _act(act), _dense(w2, "w2", dt, hidden, dim, dev), _vec(b2, "b2", dt, dim, dev),
-                              _dense(out, "out", dt, rows, dim, dev), _ptr(ws), ws.numel() * ws.element_size(), _ptr(dev_status), _stream()),
+    _check(lib.toma_mlp_layer(rows, dim, hidden, code, _dense(x, "x", dt, (rows, dim), dev), _dense(delta, "delta", dt, (rows, dim), dev),
+                              _vec(norm_weight, "norm_weight", dt, dim, dev), eps, _dense(w1, "w1", dt, (dim, hidden), dev),
+                              _vec(b1, "b1", dt, hidden, dev), _act(act), _dense(w2, "w2", dt, (hidden, dim), dev), _vec(b2, "b2", dt, dim, dev),
+                              _dense(out, "out", dt, (rows, dim), dev), _ptr(ws), ws.numel() * ws.element_size(), _ptr(dev_status), _stream()),
            "toma_mlp_layer")
 
 

@@ -151,6 +151,9 @@ struct LinearPlusOp {
 // the contraction (6, 7, 8).  `steps`: of 128 bytes of a row; at2, at4, at8: clusters of the device at once.
 int linear_plus_form(int M, int N, int steps, int sms, int pairs, int at2, int at4, int at8);
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
+// At most 16 rows, `split` CTAs (1, 2, 4 or 8) for the contraction of 64 columns.
+int linear_rows_split(int N, int steps, int sms);
+cudaError_t launch_linear_rows(const LinearPlusOp& o, int split, cudaStream_t s);
 cudaError_t launch_linear_plus_simt(const LinearPlusOp& o, cudaStream_t s);  // fp32
 // w [K][N] bf16 -> q [N][K] e4m3 (row stride ldq) with scale [N].
 cudaError_t launch_quantise_weight(int K, int N, const void* w, void* q, int ldq, float* scale, cudaStream_t s);

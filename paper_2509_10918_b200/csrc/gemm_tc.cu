@@ -15,11 +15,13 @@
 #include <climits>
 
 #include "common.cuh"
+#include "linear_epilogue.cuh"
 #include "tc.cuh"
 
 namespace toma {
 
 using namespace tc;
+using namespace epi;
 
 namespace {
 
@@ -27,20 +29,9 @@ constexpr int kKC = 64;                  // contraction elements per stage
 constexpr int kSlab = kKC * 128;         // [64 k][64 n] slab of W, 128-byte rows
 constexpr int kABytes = 128 * 128;       // [128 m][64 k] slab of A
 
-// What a kernel multiplies and what it does with the sums.  kPlain: bf16, up to three matrices, an activation.  kPlus: bf16, one
-// matrix, bias, activation and residual.  kPlus8: the same of e4m3 operands with scales.  A row of a stage is 128 bytes of either
-// type, so e4m3 takes the same slabs, boxes and cycles with twice the contraction elements; W is K-major there, [n][k] as stored.
-constexpr int kPlain = 0, kPlus = 1, kPlus8 = 2;
+// Contraction elements of a stage, and of an MMA (32 bytes).
 template <int kKind> constexpr int kStepK = kKind == kPlus8 ? 2 * kKC : kKC;   // contraction elements per stage
 template <int kKind> constexpr int kMmaK = kKind == kPlus8 ? 32 : 16;          // ... per MMA (32 bytes)
-
-// The epilogue of kPlus and kPlus8.  bias, a_scale, w_scale: [n], [m], [n], residual: [m][n], each or none.
-struct LinearPlus {
-  const __nv_bfloat16 *bias, *residual;
-  const float *a_scale, *w_scale;
-  __nv_bfloat16* c;
-  int ldc, ldr;
-};
 
 // The maps of a stage's slab j of W, and the MMAs of a stage.
 template <int kKind>
@@ -58,60 +49,6 @@ __device__ __forceinline__ constexpr uint32_t idesc_of(int M, int N) {
   return kKind == kPlus8 ? idesc_f16(kFmtE4M3, kFmtE4M3, false, false, M, N) : idesc_f16(kFmtBF16, kFmtBF16, false, true, M, N);
 }
 
-// GELU(v) = v Phi(v) = max(v, 0) - |v| Phi(-|v|) of two values, for results that are rounded to bf16.
-// Phi(-a) = erfcx(a / sqrt 2) / 2 * 2^(-a^2 log2(e) / 2), and erfcx(x) / 2 = t (c0 + c1 t + ... + c7 t^7) with
-// t = 1 / (1 + 0.33 x): the coefficients are the minimax fit of the relative error on x in [0, 10] (9.4e-8; with fp32
-// arithmetic the result is within 5e-7 of the exact one for v > -1 and 8e-6 down to -13, where v (1 + erff) loses all
-// digits).  Eleven issue slots and two MUFU operations per value against about 45 slots with erff, which made the first
-// layer of an MLP of 4096 x 2560 x 640 a matter of its epilogue (34 us of which 13 us the activation).
-__device__ __forceinline__ float rcp_mufu(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float min_nan(float a, float b) {  // a number that is none stays one
-  float d;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t both(float v) { return pack2(v, v); }
-__device__ __forceinline__ void gelu2(uint32_t& v0, uint32_t& v1) {
-  const float x0 = __uint_as_float(v0), x1 = __uint_as_float(v1);
-  const uint64_t a = pack2(min_nan(fabsf(x0), 30.f), min_nan(fabsf(x1), 30.f));
-  float d0, d1, e0, e1;
-  unpack2(fma2(a, both(0.233345238f), both(1.f)), d0, d1);
-  const uint64_t t = pack2(rcp_mufu(d0), rcp_mufu(d1));
-  uint64_t q = fma2(both(-0.0676728131f), t, both(0.230118425f));
-  q = fma2(q, t, both(-0.175574611f));
-  q = fma2(q, t, both(0.204249755f));
-  q = fma2(q, t, both(0.0236104601f));
-  q = fma2(q, t, both(0.100611901f));
-  q = fma2(q, t, both(0.0914779779f));
-  q = fma2(q, t, both(0.0931789011f));
-  unpack2(mul2(mul2(a, both(-0.72134752f)), a), e0, e1);
-  q = mul2(mul2(mul2(q, t), a), pack2(ex2_mufu(e0), ex2_mufu(e1)));
-  float g0, g1;
-  unpack2(sub2(pack2(fmaxf(x0, 0.f), fmaxf(x1, 0.f)), q), g0, g1);
-  v0 = __float_as_uint(g0);
-  v1 = __float_as_uint(g1);
-}
-// v sigmoid(z) = v / (1 + 2^(-z log2(e))) of two values, with z = v (SiLU) or z = 2 sqrt(2 / pi) (v + 0.044715 v^3) (GELU by tanh:
-// (1 + tanh u) / 2 = sigmoid(2 u)).  The approximate exponential and reciprocal are within 2^-21 of it, far below the rounding
-// to bf16.  (A none-number in v stays one through the product with v.)
-template <int kAct>
-__device__ __forceinline__ void by_sigmoid2(uint32_t& v0, uint32_t& v1) {
-  const uint64_t v = pack2(__uint_as_float(v0), __uint_as_float(v1));
-  uint64_t z;
-  if constexpr (kAct == kActSilu) z = mul2(v, both(-1.44269504f));
-  else z = mul2(v, fma2(mul2(v, v), both(-0.102943240f), both(-2.30220819f)));
-  float z0, z1, d0, d1;
-  unpack2(z, z0, z1);
-  unpack2(add2(pack2(ex2_mufu(z0), ex2_mufu(z1)), both(1.f)), d0, d1);
-  float y0, y1;
-  unpack2(mul2(v, pack2(rcp_mufu(d0), rcp_mufu(d1))), y0, y1);
-  v0 = __float_as_uint(y0);
-  v1 = __float_as_uint(y1);
-}
 // One branch for 32 values: a branch for each pair makes a chain of their latencies (16384 x 5120 x 1280 in 8 bits 191 us so).
 __device__ __forceinline__ void activate32(uint32_t (&r)[32], int act) {
   if (act == kActGelu) {
@@ -125,19 +62,6 @@ __device__ __forceinline__ void activate32(uint32_t (&r)[32], int act) {
     for (int e = 0; e < 32; e += 2) by_sigmoid2<kActGeluTanh>(r[e], r[e + 1]);
   }
 }
-// r += 2 e, 2 e + 1: eight bf16 of a packet.
-__device__ __forceinline__ void add_packet(uint32_t* r, const uint4& b) {
-  const uint32_t bb[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    float lo, hi;
-    unpack2(add2(pack2(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1])), pack2(__uint_as_float(bb[u] << 16), __uint_as_float(bb[u] & 0xFFFF0000u))),
-            lo, hi);
-    r[2 * u] = __float_as_uint(lo);
-    r[2 * u + 1] = __float_as_uint(hi);
-  }
-}
-
 // ------------------------------------------------------------------------------------------------
 // Persistent form: one CTA per SM walks over tiles of 128 rows x kCols columns.  The ring runs on across tiles, and two
 // accumulators in tensor memory alternate, so that a tile's epilogue (eight warps: a GELU per element is as long as the
@@ -684,35 +608,6 @@ struct SplitBars {
   int abort_flag;
 };
 static_assert(sizeof(SplitBars) <= 256, "barrier block outgrew its reservation");
-__device__ __forceinline__ void st_peer_v4(uint32_t addr, const uint32_t* v) {
-  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
-// The epilogue of eight columns of one row, into global memory.
-template <int kKind>
-__device__ __forceinline__ void finish8(float (&v)[8], float row_scale, const LinearPlus& p, int act, const uint4& res, int n, __nv_bfloat16* c) {
-  uint32_t r[8];
-  if constexpr (kKind == kPlus8) {
-    const float4 s0 = *reinterpret_cast<const float4*>(p.w_scale + n), s1 = *reinterpret_cast<const float4*>(p.w_scale + n + 4);
-    const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= row_scale * s[e];
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(v[e]);
-  if (p.bias) add_packet(r, *reinterpret_cast<const uint4*>(p.bias + n));
-#pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    if (act == kActGelu) gelu2(r[e], r[e + 1]);
-    else if (act == kActSilu) by_sigmoid2<kActSilu>(r[e], r[e + 1]);
-    else if (act == kActGeluTanh) by_sigmoid2<kActGeluTanh>(r[e], r[e + 1]);
-  }
-  if (p.residual) add_packet(r, res);
-  __align__(16) __nv_bfloat162 q[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1]));
-  *reinterpret_cast<uint4*>(c) = *reinterpret_cast<const uint4*>(q);
-}
-
 template <int kKind, int S>
 __global__ void __launch_bounds__((2 + kEpiWarps) * 32, 1)
 linear_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, int M, int N, int K, int act,
@@ -934,7 +829,7 @@ cudaError_t run_plus(const LinearPlusOp& o, const CUtensorMap& ta, const CUtenso
   const int at_once = pairs_at_once(), steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
   const int at2 = splits_at_once<kKind, 2>(), at4 = splits_at_once<kKind, 4>(), at8 = splits_at_once<kKind, 8>();
   int form = linear_plus_form(o.M, o.N, steps, sm_count(), at_once, at2, at4, at8);
-  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed)) {  // test-only override
+  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 1 && v <= 8) {  // test-only override
     const bool pair = v == 3 || v == 5, split = v >= 6 && v <= 8;
     if (pair ? o.M > 128 && at_once > 0 : !split || (steps >= 1 << (v - 5) && (v == 6 ? at2 : v == 7 ? at4 : at8) > 0)) form = v;
   }
@@ -958,6 +853,8 @@ int linear_plus_form(int M, int N, int steps, int sms, int pairs, int at2, int a
 
 // c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
+  const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
+  if (o.M <= 16 && (tune == 0 || tune == 9)) return launch_linear_rows(o, linear_rows_split(o.N, (o.K + (o.f8 ? 63 : 31)) / (o.f8 ? 64 : 32), sm_count()), s);
   CUtensorMap ta, tw;
   const uint64_t adims[2] = {(uint64_t)o.K, (uint64_t)o.M}, astr[1] = {(uint64_t)o.lda * (o.f8 ? 1 : 2)};
   const uint32_t abox[2] = {o.f8 ? 128u : 64u, 128};

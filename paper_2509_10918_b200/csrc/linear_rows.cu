@@ -1,0 +1,197 @@
+// c = act(a w + bias) + residual for at most 16 rows of a: a modulation vector out of a time embedding, a single token.
+//
+// What there is to do is to read w once: 2 m <= 32 multiply-adds per weight are far below what the SMs have, and tiles of 128
+// rows leave most SMs without a tile.  So 64 columns of w are a cluster's, its CTAs split the contraction between them and their
+// eight warps split it further, with no staging in shared memory: a weight goes from global memory into the operand registers of
+// an mma.sync (the legacy tensor path, whose rate does not matter here: 32 columns of 16 padded rows take 16 instructions per 2 KB
+// of weights).  The order of the contraction elements inside an instruction is free as long as both operands use the same, and is
+// chosen so that a thread's elements are consecutive in memory:
+//   bf16, w [k][n]: 32 elements at a time, thread t of four has elements 8 t .. 8 t + 7, each as 16 bytes of a row of w (eight columns,
+//   one of each of eight instructions: columns 8 g + j form instruction j), paired by byte permutations; of a it has 16 bytes.
+//   e4m3, w [n][k]: 64 elements at a time, thread t has elements 16 t .. 16 t + 15, 16 bytes of a column, and of a row of a.
+// The warps' sums are added up through shared memory, the CTAs' through distributed shared memory, in a fixed order.
+// 2 x 5120 x 1280 in bf16 (13 MB of weights, out of L2): TODO us.
+#include "linear_epilogue.cuh"
+
+namespace toma {
+
+using namespace tc;
+using namespace epi;
+
+namespace {
+
+constexpr int kWarps = 8, kBlock = 64, kPitch = kBlock + 4;
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 load16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ uint4 none16() { return make_uint4(0, 0, 0, 0); }
+// 16 bytes of a row of e4m3, `left` (a multiple of 8) of them real; nothing behind them is read.
+__device__ __forceinline__ uint4 load16_e4m3(const uint8_t* p, int left) {
+  if (left >= 16) return load16(p);
+  if (left < 8) return none16();
+  const uint2 q = *reinterpret_cast<const uint2*>(p);
+  return make_uint4(q.x, q.y, 0, 0);
+}
+__device__ __forceinline__ uint32_t word(const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
+
+struct RowsOp {
+  const void *a, *w;
+  int lda, ldw, M, N, K, act, split;
+};
+
+// The operands of one step: eight packets of w, the packets of rows g and g + 8 of a.
+template <int kKind, bool kTall>
+struct Step {
+  uint4 w[8], a[kTall ? 2 : 1];
+  __device__ __forceinline__ void load(const RowsOp& o, int step, int n0, int g, int t, bool there) {
+    if constexpr (kKind == kPlus8) {
+      const int k = step * 64 + 16 * t, left = there ? o.K - k : 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int n = n0 + 8 * j + g;
+        w[j] = load16_e4m3((const uint8_t*)o.w + (size_t)n * o.ldw + k, n < o.N ? left : 0);
+      }
+#pragma unroll
+      for (int i = 0; i < (kTall ? 2 : 1); ++i) a[i] = load16_e4m3((const uint8_t*)o.a + (size_t)(g + 8 * i) * o.lda + k, g + 8 * i < o.M ? left : 0);
+    } else {
+      const int k = step * 32 + 8 * t;
+      const bool in_k = there && k < o.K;
+      const __nv_bfloat16* at = (const __nv_bfloat16*)o.w + (size_t)k * o.N + n0 + 8 * g;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = in_k && n0 + 8 * g < o.N ? load16(at + (size_t)j * o.N) : none16();
+#pragma unroll
+      for (int i = 0; i < (kTall ? 2 : 1); ++i)
+        a[i] = in_k && g + 8 * i < o.M ? load16((const __nv_bfloat16*)o.a + (size_t)(g + 8 * i) * o.lda + k) : none16();
+    }
+  }
+  __device__ __forceinline__ void multiply(float (&acc)[8][4]) const {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint32_t a0 = word(a[0], 2 * s), a2 = word(a[0], 2 * s + 1), a1 = kTall ? word(a[kTall ? 1 : 0], 2 * s) : 0, a3 = kTall ? word(a[kTall ? 1 : 0], 2 * s + 1) : 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (kKind == kPlus8) {
+          mma_e4m3(acc[j], a0, a1, a2, a3, word(w[j], 2 * s), word(w[j], 2 * s + 1));
+        } else {
+          const uint32_t pick = j % 2 ? 0x7632 : 0x5410;  // the column's half of two rows' words
+          mma_bf16(acc[j], a0, a1, a2, a3, __byte_perm(word(w[4 * s], j / 2), word(w[4 * s + 1], j / 2), pick),
+                   __byte_perm(word(w[4 * s + 2], j / 2), word(w[4 * s + 3], j / 2), pick));
+        }
+      }
+    }
+  }
+};
+
+template <int kKind, bool kTall>
+__global__ void __launch_bounds__(kWarps * 32, 2) linear_rows_kernel(const RowsOp o, const LinearPlus plus) {
+  constexpr int kRows = kTall ? 16 : 8;
+  __shared__ __align__(16) float part[kWarps][kRows][kPitch];
+  __shared__ __align__(16) float sums[8][kRows][8];  // [rank][row] eights of columns that this CTA finishes, 8 / split of them
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int rank = o.split > 1 ? (int)cluster_rank() : 0, n0 = (int)(blockIdx.x / o.split) * kBlock;
+  const int steps = (o.K + (kKind == kPlus8 ? 63 : 31)) / (kKind == kPlus8 ? 64 : 32), parts = kWarps * o.split, p = rank * kWarps + warp;
+  const int first = (int)((long long)steps * p / parts), last = (int)((long long)steps * (p + 1) / parts);
+  dependency_wait();
+  if (threadIdx.x == 0) release_dependents();
+  if (o.split > 1) cluster_arrive();
+
+  // rows x 8 threads finish: an eight of columns of a row each, of the eights that are this CTA's
+  const int row = threadIdx.x >> 3, oct = threadIdx.x & 7, per = 8 / o.split, n = n0 + oct * 8;
+  const bool mine = row < o.M && row < kRows && oct / per == rank && n < o.N;
+  uint4 res = none16();
+  float acc[8][4] = {};
+  Step<kKind, kTall> s0, s1;
+  s0.load(o, first, n0, g, t, first < last);
+  s1.load(o, first + 1, n0, g, t, first + 1 < last);
+  if (mine && plus.residual) res = load16(plus.residual + (size_t)row * plus.ldr + n);
+  for (int k = first; k < last; k += 2) {
+    s0.multiply(acc);
+    if (k + 2 < last) s0.load(o, k + 2, n0, g, t, true);
+    if (k + 1 < last) s1.multiply(acc);
+    if (k + 3 < last) s1.load(o, k + 3, n0, g, t, true);
+  }
+#pragma unroll
+  for (int i = 0; i < (kTall ? 2 : 1); ++i) {
+    float* at = part[warp][g + 8 * i];
+    if constexpr (kKind == kPlus8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) *reinterpret_cast<float2*>(at + 8 * j + 2 * t) = make_float2(acc[j][2 * i], acc[j][2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {  // columns 8 (2 t + h) + j
+        *reinterpret_cast<float4*>(at + 16 * t + 8 * h) = make_float4(acc[0][2 * i + h], acc[1][2 * i + h], acc[2][2 * i + h], acc[3][2 * i + h]);
+        *reinterpret_cast<float4*>(at + 16 * t + 8 * h + 4) = make_float4(acc[4][2 * i + h], acc[5][2 * i + h], acc[6][2 * i + h], acc[7][2 * i + h]);
+      }
+    }
+  }
+  __syncthreads();
+  float v[8] = {};
+  if (row < kRows) {
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(&part[w][row][oct * 8]), y = *reinterpret_cast<const float4*>(&part[w][row][oct * 8 + 4]);
+      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+    }
+  }
+  if (o.split > 1) {
+    cluster_wait();  // all CTAs have begun
+    if (row < kRows) {
+      // to who finishes this eight, which has per of them a row
+      const uint32_t at = peer_addr(smem_u32(&sums[0][0][0]) + (uint32_t)(((rank * kRows + row) * per + oct % per) * 32), (uint32_t)(oct / per));
+      uint32_t b[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(v[e]);
+      st_peer_v4(at, b);
+      st_peer_v4(at + 16, b + 4);
+    }
+    cluster_arrive();
+    cluster_wait();  // all sums are there, and nobody writes into another's any more
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    if (mine) {
+      for (int r = 0; r < o.split; ++r) {
+        const float* at = &sums[0][0][0] + ((r * kRows + row) * per + oct % per) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += at[e];
+      }
+    }
+  }
+  if (mine) finish8<kKind>(v, kKind == kPlus8 ? plus.a_scale[row] : 1.f, plus, o.act, res, n, plus.c + (size_t)row * plus.ldc + n);
+}
+
+template <int kKind, bool kTall>
+cudaError_t run_rows(const RowsOp& o, const LinearPlus& plus, cudaStream_t s) {
+  const dim3 grid((unsigned)((o.N + kBlock - 1) / kBlock) * o.split), block(kWarps * 32);
+  return o.split > 1 ? launch_dependent_cluster(linear_rows_kernel<kKind, kTall>, grid, block, 0, o.split, s, o, plus)
+                     : launch_dependent(linear_rows_kernel<kKind, kTall>, grid, block, 0, s, o, plus);
+}
+
+}  // namespace
+
+// CTAs that split a block's contraction: twice the SMs in all at most, with a step for every warp.
+int linear_rows_split(int N, int steps, int sms) {
+  const int blocks = (N + kBlock - 1) / kBlock;
+  int split = 1;
+  while (split < 8 && blocks * split * 2 <= 2 * sms && steps >= kWarps * split) split *= 2;
+  return split;
+}
+
+cudaError_t launch_linear_rows(const LinearPlusOp& l, int split, cudaStream_t s) {
+  const LinearPlus plus{(const __nv_bfloat16*)l.bias, (const __nv_bfloat16*)l.residual, l.a_scale, l.w_scale, (__nv_bfloat16*)l.c, l.ldc, l.ldr};
+  const RowsOp o{l.a, l.w, l.lda, l.ldw, l.M, l.N, l.K, l.act, split};
+  const cudaError_t e = l.f8 ? (l.M > 8 ? run_rows<kPlus8, true>(o, plus, s) : run_rows<kPlus8, false>(o, plus, s))
+                             : (l.M > 8 ? run_rows<kPlus, true>(o, plus, s) : run_rows<kPlus, false>(o, plus, s));
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace toma
