@@ -44,6 +44,12 @@ __device__ __forceinline__ uint64_t w_desc(uint32_t wa, int kk) {
   if constexpr (kKind == kPlus8) return smem_desc_sw128(wa + kk * 32, 16, 1024);
   else return smem_desc_sw128(wa + kk * 2048, kSlab, 1024);
 }
+// Half a slab: 32 columns, rows of 64 bytes in bf16.
+template <int kKind>
+__device__ __forceinline__ uint64_t half_desc(uint32_t wa, int kk) {
+  if constexpr (kKind == kPlus8) return smem_desc_sw128(wa + kk * 32, 16, 1024);
+  else return smem_desc_sw64(wa + kk * 1024, 16, 512);
+}
 template <int kKind>
 __device__ __forceinline__ constexpr uint32_t idesc_of(int M, int N) {
   return kKind == kPlus8 ? idesc_f16(kFmtE4M3, kFmtE4M3, false, false, M, N) : idesc_f16(kFmtBF16, kFmtBF16, false, true, M, N);
@@ -76,7 +82,7 @@ template <int kCols, int kKind> constexpr int kOutWarps = kKind == kPlain ? kEpi
 struct PersistBars {
   uint64_t full[kMaxStages], empty[kMaxStages];
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t res[16];  // kPlus: the residual's slab of an epilogue warp is there
+  uint64_t res[20];  // kPlus: the residual's slab of an epilogue warp is there
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -247,7 +253,7 @@ linear_persistent_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_
       mbar_init(&bar->acc_empty[a], kOutWarps<kCols, kKind>);
     }
     if constexpr (kKind != kPlain)
-      for (int e = 0; e < 16; ++e) mbar_init(&bar->res[e], 1);
+      for (int e = 0; e < kOutWarps<kCols, kKind>; ++e) mbar_init(&bar->res[e], 1);
     bar->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tm_a);
@@ -357,19 +363,24 @@ constexpr int kPairRows = 256, kPairCols = 256;
 // others of 13 to 37 row blocks 3 % slower with panels of twelve and a rest).
 constexpr int kPanel = 12;
 // With bias and residual there is a form of 256 x 128 besides: a CTA keeps 64 of the columns of W, half the work per tile and so
-// less of it left over where the tiles of a launch do not come out even.
+// less of it left over where the tiles of a launch do not come out even; and one of 256 x 320, whose tiles divide the widths of these
+// models' layers (multiples of 320) and read 36 KB per SM for 1.25 times the multiply-adds of 32.  Its 64 columns behind the 256 are an
+// MMA of their own (32 in each CTA, half a slab: 64-byte rows in bf16, 32 rows in e4m3), and it has one accumulator, whose
+// epilogue nothing overlaps but the loads of the next tile's first stages.
 template <int kCols, int kKind>
 struct PairCfg {
   static constexpr int kSlabs = kCols / 128;                        // of W in a CTA
-  static constexpr int kStageBytes = kABytes + kSlabs * kSlab;      // a CTA's half
-  static constexpr int kStages = kKind == kPlain ? 6 : kCols == 256 ? 5 : 8;
+  static constexpr bool kMore = kCols == 320;                       // ... and half a slab
+  static constexpr int kStageBytes = kABytes + kSlabs * kSlab + (kMore ? kSlab / 2 : 0);  // a CTA's half
+  static constexpr int kStages = kKind == kPlain ? 6 : kMore ? 4 : kCols == 256 ? 5 : 8;
+  static constexpr int kAccs = kMore ? 1 : 2;                       // accumulators in tensor memory
   static constexpr int kStaging = kOutWarps<kCols, kKind> * 32 * 128;
   static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
 };
 struct PairBars {
   uint64_t full[8], empty[8];  // (full: of the first CTA)
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t res[16];  // kPlus: the residual's slab of an epilogue warp is there
+  uint64_t res[20];  // kPlus: the residual's slab of an epilogue warp is there
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -413,7 +424,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       mbar_init(&bar->acc_empty[a], 2 * kOutWarps<kCols, kKind>);
     }
     if constexpr (kKind != kPlain)
-      for (int e = 0; e < 16; ++e) mbar_init(&bar->res[e], 1);
+      for (int e = 0; e < kOutWarps<kCols, kKind>; ++e) mbar_init(&bar->res[e], 1);
     bar->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tm_a);
@@ -437,7 +448,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       for (int item = pair; ok && item < n_items; item += pairs) {
         int m0, n0, z;
         place(item, m0, n0, z);
-        m0 += rank * 128, n0 += rank * (kCols / 2);  // this CTA's rows and columns
+        const int more = n0 + 256 + rank * 32;
+        m0 += rank * 128, n0 += rank * (C::kMore ? 128 : kCols / 2);  // this CTA's rows and columns
         const CUtensorMap* tm_w = z == 0 ? &tm_w0 : z == 1 ? &tm_w1 : &tm_w2;
         for (int k = 0; k < nk; ++k, ++kc) {
           const int s = kc % kStages;
@@ -449,18 +461,22 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             if constexpr (kKind == kPlus8) tma_load_2d_pair(sa + kABytes + j * kSlab, tm_w, &bar->full[s], k * kStepK<kKind>, n0 + j * 64);
             else tma_load_2d_pair(sa + kABytes + j * kSlab, tm_w, &bar->full[s], n0 + j * 64, k * kKC);
           }
+          if constexpr (C::kMore) {
+            if constexpr (kKind == kPlus8) tma_load_2d_pair(sa + kABytes + C::kSlabs * kSlab, &tm_w2, &bar->full[s], k * kStepK<kKind>, more);
+            else tma_load_2d_pair(sa + kABytes + C::kSlabs * kSlab, &tm_w2, &bar->full[s], more, k * kKC);
+          }
         }
       }
     }
   } else if (warp == 1) {
     if (rank == 0) {
       if (elect_one()) {
-        constexpr uint32_t idesc = idesc_of<kKind>(kPairRows, kCols);
+        constexpr uint32_t idesc = idesc_of<kKind>(kPairRows, C::kMore ? 256 : kCols), idesc_more = idesc_of<kKind>(kPairRows, 64);
         int kc = 0, n = 0;
         bool ok = true;
         for (int item = pair; ok && item < n_items; item += pairs, ++n) {
-          const int a = n & 1;
-          if (n >= 2 && !mbar_wait(&bar->acc_empty[a], ((n >> 1) - 1) & 1, dev_status, abort_flag)) break;
+          const int a = n % C::kAccs;
+          if (n >= C::kAccs && !mbar_wait(&bar->acc_empty[a], (n / C::kAccs - 1) & 1, dev_status, abort_flag)) break;
           tc_fence_after();
           for (int k = 0; k < nk; ++k, ++kc) {
             const int s = kc % kStages;
@@ -469,8 +485,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
             const uint32_t aa = smem_u32(smem + s * C::kStageBytes), wa = aa + kABytes;
             // (32 bytes of contraction elements per MMA, zero filled past K)
             const int ksteps = min(kStepK<kKind>, K - k * kStepK<kKind> + kMmaK<kKind> - 1) / kMmaK<kKind>;
-            for (int kk = 0; kk < ksteps; ++kk)
+            for (int kk = 0; kk < ksteps; ++kk) {
               mma_ss_pair<kKind == kPlus8>(tmem + a * 256, smem_desc_sw128(aa + kk * 32, 16, 1024), w_desc<kKind>(wa, kk), idesc, k > 0 || kk > 0);
+              if constexpr (C::kMore)
+                mma_ss_pair<kKind == kPlus8>(tmem + 256, smem_desc_sw128(aa + kk * 32, 16, 1024), half_desc<kKind>(wa + C::kSlabs * kSlab, kk), idesc_more,
+                                             k > 0 || kk > 0);
+            }
             mma_commit_pair(&bar->empty[s]);
           }
           if (ok) mma_commit_pair(&bar->acc_full[a]);
@@ -487,13 +507,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_consta
       int m0, n0, z;
       place(item, m0, n0, z);
       m0 += rank * 128 + quarter * 32;
-      const int a = n & 1, slabs = (min(kCols, N - n0) + 63) / 64;
+      const int a = n % C::kAccs, slabs = (min(kCols, N - n0) + 63) / 64;
       const CUtensorMap* tm_c = z == 0 ? &tm_c0 : z == 1 ? &tm_c1 : &tm_c2;
       if constexpr (kKind != kPlain) {
         if (half < slabs) plus_out.fetch(n0 + half * 64, m0);
       }
       // one answer per warp: the tensor-memory loads below are warp-wide operations
-      if (!__all_sync(0xffffffffu, mbar_wait(&bar->acc_full[a], (n >> 1) & 1, dev_status, abort_flag))) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(&bar->acc_full[a], (n / C::kAccs) & 1, dev_status, abort_flag))) break;
       tc_fence_after();
       const uint32_t taddr = tmem + a * 256 + ((uint32_t)(quarter * 32) << 16);
       if constexpr (kKind == kPlain) tile_out(taddr, mine, lane, tm_c, half, slabs, n0, m0, M, act);
@@ -582,7 +602,8 @@ cudaError_t run_form(int form, int at_once, int M, int N, int K, int n_mats, con
   else if (form == 2) e = run_persistent<192, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   else if (form == 1) e = run_persistent<256, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   if constexpr (kKind != kPlain)
-    if (form == 5) e = run_pair<128, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+    if (form == 10) e = run_pair<320, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+    else if (form == 5) e = run_pair<128, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -829,8 +850,8 @@ cudaError_t run_plus(const LinearPlusOp& o, const CUtensorMap& ta, const CUtenso
   const int at_once = pairs_at_once(), steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
   const int at2 = splits_at_once<kKind, 2>(), at4 = splits_at_once<kKind, 4>(), at8 = splits_at_once<kKind, 8>();
   int form = linear_plus_form(o.M, o.N, steps, sm_count(), at_once, at2, at4, at8);
-  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 1 && v <= 8) {  // test-only override
-    const bool pair = v == 3 || v == 5, split = v >= 6 && v <= 8;
+  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 1 && v != 9) {  // test-only override
+    const bool pair = v == 3 || v == 5 || v == 10, split = v >= 6 && v <= 8;
     if (pair ? o.M > 128 && at_once > 0 : !split || (steps >= 1 << (v - 5) && (v == 6 ? at2 : v == 7 ? at4 : at8) > 0)) form = v;
   }
   if (form == 6) return run_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
@@ -841,7 +862,13 @@ cudaError_t run_plus(const LinearPlusOp& o, const CUtensorMap& ta, const CUtenso
   const uint32_t cbox[2] = {64, 32};  // a warp's 32 rows of one 64-column slab
   if (!encode_tmap_16bit(&tc, o.c, 2, cdims, cstr, cbox) || (o.residual && !encode_tmap_16bit(&tr, o.residual, 2, cdims, rstr, cbox)))
     return cudaErrorInvalidValue;
-  const CUtensorMap tws[3] = {tw, tr, tw}, tcs[3] = {tc, tc, tc};
+  CUtensorMap th = tw;
+  if (form == 10) {  // half slabs of W
+    const uint64_t wdims[2] = {(uint64_t)(o.f8 ? o.K : o.N), (uint64_t)(o.f8 ? o.N : o.K)}, wstr[1] = {(uint64_t)o.ldw * (o.f8 ? 1 : 2)};
+    const uint32_t hbox[2] = {o.f8 ? 128u : 32u, o.f8 ? 32u : 64u};
+    if (!(o.f8 ? encode_tmap_8bit : encode_tmap_16bit)(&th, o.w, 2, wdims, wstr, hbox)) return cudaErrorInvalidValue;
+  }
+  const CUtensorMap tws[3] = {tw, tr, th}, tcs[3] = {tc, tc, tc};
   return run_form<kKind>(form, at_once, o.M, o.N, o.K, 1, ta, tws, tcs, o.act, plus, dev_status, s);
 }
 }  // namespace
