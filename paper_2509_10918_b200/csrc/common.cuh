@@ -147,9 +147,13 @@ struct LinearPlusOp {
   void* c;
   int lda, ldw, ldr, ldc, act;
 };
-// The form it takes on the tensor cores: linear_tc_form()'s, 256 x 128 by pairs (5), or 128 x 128 by clusters of 2, 4, 8 that split
-// the contraction (6, 7, 8).  `steps`: of 128 bytes of a row; at2, at4, at8: clusters of the device at once.
-int linear_plus_form(int M, int N, int steps, int sms, int pairs, int at2, int at4, int at8);
+// What a device holds at once: SMs, pairs, and clusters of 2, 4, 8 CTAs and of 2, 3 pairs that split a contraction.
+struct PlusDevice {
+  int sms, pairs, split[3], pair_split[2];
+};
+// The form it takes on the tensor cores: 128 x 128 (4), 128 x 192 (2), 256 x 256 (3) or 256 x 320 (5) by pairs, or, with the contraction
+// split, 128 x 128 by 2, 4, 8 CTAs (6, 7, 8) or 256 x 256 by 2, 3 pairs (9, 10).  `steps`: of 128 bytes of a row.
+int linear_plus_form(int M, int N, int steps, int act, const PlusDevice& d);
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
 // At most 16 rows, `split` CTAs (1, 2, 4 or 8) for the contraction of 64 columns.
 int linear_rows_split(int N, int steps, int sms);

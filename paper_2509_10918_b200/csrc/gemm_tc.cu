@@ -91,7 +91,7 @@ static_assert(sizeof(PersistBars) <= 512, "barrier block outgrew its reservation
 template <int kCols, int kKind>
 struct PersistCfg {
   static constexpr int kStageBytes = kABytes + kCols / 64 * kSlab;
-  static constexpr int kStages = kCols == 128 ? 6 : kKind != kPlain && kCols == 256 ? 3 : 4;
+  static constexpr int kStages = kCols == 128 ? 6 : 4;
   static constexpr int kStaging = kOutWarps<kCols, kKind> * 32 * 128;  // per epilogue warp: 32 rows of a 64-column slab
   static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
   static constexpr uint32_t kAccCols = kCols == 128 ? 128 : 256;
@@ -362,9 +362,8 @@ constexpr int kPairRows = 256, kPairCols = 256;
 // to 1 and 2 % more than 12.  Twelve at most, all panels of a matrix alike: a last one of a few rows shares nothing (6585 x 8448 x 2112 and
 // others of 13 to 37 row blocks 3 % slower with panels of twelve and a rest).
 constexpr int kPanel = 12;
-// With bias and residual there is a form of 256 x 128 besides: a CTA keeps 64 of the columns of W, half the work per tile and so
-// less of it left over where the tiles of a launch do not come out even; and one of 256 x 320, whose tiles divide the widths of these
-// models' layers (multiples of 320) and read 36 KB per SM for 1.25 times the multiply-adds of 32.  Its 64 columns behind the 256 are an
+// With bias and residual there is a form of 256 x 320 besides, whose tiles divide the widths of these models' layers (multiples of
+// 320) and read 36 KB per SM for 1.25 times the multiply-adds of 32.  Its 64 columns behind the 256 are an
 // MMA of their own (32 in each CTA, half a slab: 64-byte rows in bf16, 32 rows in e4m3), and it has one accumulator, whose
 // epilogue nothing overlaps but the loads of the next tile's first stages.
 template <int kCols, int kKind>
@@ -372,13 +371,13 @@ struct PairCfg {
   static constexpr int kSlabs = kCols / 128;                        // of W in a CTA
   static constexpr bool kMore = kCols == 320;                       // ... and half a slab
   static constexpr int kStageBytes = kABytes + kSlabs * kSlab + (kMore ? kSlab / 2 : 0);  // a CTA's half
-  static constexpr int kStages = kKind == kPlain ? 6 : kMore ? 4 : kCols == 256 ? 5 : 8;
+  static constexpr int kStages = kKind == kPlain ? 6 : kMore ? 4 : 5;
   static constexpr int kAccs = kMore ? 1 : 2;                       // accumulators in tensor memory
   static constexpr int kStaging = kOutWarps<kCols, kKind> * 32 * 128;
   static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStaging + 512;
 };
 struct PairBars {
-  uint64_t full[8], empty[8];  // (full: of the first CTA)
+  uint64_t full[6], empty[6];  // (full: of the first CTA)
   uint64_t acc_full[2], acc_empty[2];
   uint64_t res[20];  // kPlus: the residual's slab of an epilogue warp is there
   uint32_t tmem_base;
@@ -549,34 +548,42 @@ cudaError_t run_persistent(int M, int N, int K, int n_mats, const CUtensorMap& t
                           tw[2], tc[0], tc[1], tc[2], M, N, K, (int)items, act, dev_status, plus);
 }
 
-// How many pairs the device holds at once: 0 where it places no cluster of this size (asked once per device; the other forms
-// need none).
-int pairs_at_once() {
-  static std::atomic<unsigned long long> raised{0};
-  static std::atomic<int> known[64];  // per device: 0 unknown, else the answer + 1
+// How many clusters of `ctas` CTAs of a kernel the device holds at once (asked once per device; 0: none).
+struct ClusterState {
+  std::atomic<unsigned long long> raised{0};
+  std::atomic<int> known[64];  // per device: 0 unknown, else the answer + 1
+};
+template <typename Kernel>
+int clusters_at_once(Kernel kernel, ClusterState& st, int ctas, int threads, int smem) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (const int k = known[dev].load(std::memory_order_relaxed)) return k - 1;
+  if (const int k = st.known[dev].load(std::memory_order_relaxed)) return k - 1;
   int clusters = 0;
-  bool ok = raise_dynamic_smem(linear_pair_kernel<kPlain, kPairCols>, PairCfg<kPairCols, kPlain>::kSmemBytes, raised) == cudaSuccess;
+  bool ok = raise_dynamic_smem(kernel, smem, st.raised) == cudaSuccess;
   if (ok) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2);
-    cfg.blockDim = dim3((2 + kEpiWarps) * 32);
-    cfg.dynamicSmemBytes = PairCfg<kPairCols, kPlain>::kSmemBytes;
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.x = ctas;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    ok = cudaOccupancyMaxActiveClusters(&clusters, linear_pair_kernel<kPlain, kPairCols>, &cfg) == cudaSuccess;
+    ok = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess;
   }
   if (!ok) (void)cudaGetLastError();  // a failed query is an answer, not an error of the caller's stream
   if (!ok || clusters < 0) clusters = 0;
-  known[dev].store(clusters + 1, std::memory_order_relaxed);
+  st.known[dev].store(clusters + 1, std::memory_order_relaxed);
   return clusters;
+}
+
+// How many pairs the device holds at once: 0 where it places no cluster of this size (the other forms need none).
+int pairs_at_once() {
+  static ClusterState st;
+  return clusters_at_once(linear_pair_kernel<kPlain, kPairCols>, st, 2, (2 + kEpiWarps) * 32, PairCfg<kPairCols, kPlain>::kSmemBytes);
 }
 
 template <int kCols, int kKind>
@@ -600,10 +607,10 @@ cudaError_t run_form(int form, int at_once, int M, int N, int K, int n_mats, con
   if (form == 4) e = run_persistent<128, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   else if (form == 3) e = run_pair<kPairCols, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   else if (form == 2) e = run_persistent<192, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
-  else if (form == 1) e = run_persistent<256, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+  if constexpr (kKind == kPlain)
+    if (form == 1) e = run_persistent<256, kKind>(M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   if constexpr (kKind != kPlain)
-    if (form == 10) e = run_pair<320, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
-    else if (form == 5) e = run_pair<128, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
+    if (form == 5) e = run_pair<320, kKind>(at_once, M, N, K, n_mats, ta, tw, tc, act, plus, dev_status, s);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -762,42 +769,208 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   }
 }
 
-// How many clusters of S the device holds at once (asked once per device; 0: none).
+// ------------------------------------------------------------------------------------------------
+// The same by pairs of SMs for more rows: a cluster of S pairs (S = 2, 3) splits the contraction of one tile of 256 x 256.  Eight
+// parts of 32 columns are dealt out to the pairs to finish, part u to pair u S / 8; a CTA has 128 of the rows, as in its
+// accumulator, so partial sums go between CTAs of the same half.  They have room of their own, since a peer may still multiply when
+// this pair is through.
+// ------------------------------------------------------------------------------------------------
+template <int S>
+struct PairSplitCfg {
+  static constexpr int kStages = S == 2 ? 5 : 4;
+  static constexpr int kStageBytes = kABytes + 2 * kSlab;
+  static constexpr int kMost = S == 2 ? 4 : 3;          // parts that a pair finishes, at most
+  static constexpr int kParts = (S - 1) * kMost * 32 * 128 * 4;
+  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kParts + 256;
+  static constexpr int kWarps = 16;
+};
+struct PairSplitBars {
+  uint64_t full[5], empty[5], acc_full;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(PairSplitBars) <= 256, "barrier block outgrew its reservation");
+
+template <int kKind, int S>
+__global__ void __launch_bounds__((2 + PairSplitCfg<S>::kWarps) * 32, 1)
+linear_pair_split_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w, int M, int N, int K, int act,
+                         uint32_t* dev_status, const LinearPlus plus) {
+  using C = PairSplitCfg<S>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* parts = smem + C::kStages * C::kStageBytes;  // [other pair][part][column / 4][row] packets of four columns
+  PairSplitBars* bar = reinterpret_cast<PairSplitBars*>(parts + C::kParts);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_rank(), pair = rank >> 1, side = rank & 1, leader = rank & ~1, tile = blockIdx.x / (2 * S);
+  const int nk = (K + kStepK<kKind> - 1) / kStepK<kKind>, k_first = pair * nk / S, k_last = (pair + 1) * nk / S;  // (nk >= S)
+  const int mb = (M + 255) / 256, m0 = tile % mb * 256 + side * 128, n0 = tile / mb * 256;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(&bar->full[s], 1);
+      mbar_init(&bar->empty[s], 1);
+    }
+    mbar_init(&bar->acc_full, 1);
+    bar->abort_flag = 0;
+    mbar_fence_init();
+    prefetch_tmap(&tm_a);
+    prefetch_tmap(&tm_w);
+  }
+  cluster_sync();  // all CTAs' barriers and shared memory are there
+  dependency_wait();
+  if (threadIdx.x == 0) release_dependents();
+  if (warp == 1) tmem_alloc_pair(&bar->tmem_base, 256);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bar->tmem_base;
+  volatile int* abort_flag = &bar->abort_flag;
+  const int quarter = warp & 3, group = (warp - 2) >> 2, row = quarter * 32 + lane, m = m0 + row;
+  const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+  const bool out = warp >= 2 && m0 + quarter * 32 < M;
+  bool ok = true;
+
+  if (warp == 0) {
+    if (elect_one()) {
+      for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
+        const int s = i % C::kStages;
+        if (i >= C::kStages && !mbar_wait(&bar->empty[s], ((i / C::kStages) - 1) & 1, dev_status, abort_flag)) break;
+        uint8_t* sa = smem + s * C::kStageBytes;
+        if (side == 0) mbar_expect_tx(&bar->full[s], 2 * C::kStageBytes);  // what lies past M or N comes as zeros and counts
+        const uint32_t full = peer_addr(smem_u32(&bar->full[s]), (uint32_t)leader);
+        tma_load_2d_pair_at(sa, &tm_a, full, k * kStepK<kKind>, m0);
+        for (int j = 0; j < 2; ++j) {
+          const int n = n0 + side * 128 + j * 64;
+          if constexpr (kKind == kPlus8) tma_load_2d_pair_at(sa + kABytes + j * kSlab, &tm_w, full, k * kStepK<kKind>, n);
+          else tma_load_2d_pair_at(sa + kABytes + j * kSlab, &tm_w, full, n, k * kKC);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (side == 0) {
+      if (elect_one()) {
+        constexpr uint32_t idesc = idesc_of<kKind>(256, 256);
+        const uint16_t both_ctas = (uint16_t)(3u << leader);
+        bool all = true;
+        for (int k = k_first, i = 0; k < k_last; ++k, ++i) {
+          const int s = i % C::kStages;
+          if (!mbar_wait(&bar->full[s], (i / C::kStages) & 1, dev_status, abort_flag)) { all = false; break; }
+          tc_fence_after();
+          const uint32_t aa = smem_u32(smem + s * C::kStageBytes), wa = aa + kABytes;
+          const int ksteps = min(kStepK<kKind>, K - k * kStepK<kKind> + kMmaK<kKind> - 1) / kMmaK<kKind>;
+          for (int kk = 0; kk < ksteps; ++kk)
+            mma_ss_pair<kKind == kPlus8>(tmem, smem_desc_sw128(aa + kk * 32, 16, 1024), w_desc<kKind>(wa, kk), idesc, k > k_first || kk > 0);
+          mma_commit_pair_to(&bar->empty[s], both_ctas);
+        }
+        if (all) mma_commit_pair_to(&bar->acc_full, both_ctas);
+      }
+    }
+  } else {
+    if (out) {  // what the epilogue reads besides the sums, on its way into L1
+      uint32_t x;
+      const int n = n0 + group * 64 + lane * 2;
+      if (n < N && plus.bias) asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(plus.bias + n));
+      if (kKind == kPlus8 && n < N) asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(plus.w_scale + n));
+    }
+    ok = mbar_wait_warp(&bar->acc_full, 0, dev_status, abort_flag);
+    if (ok && out) {
+      tc_fence_after();
+      // the parts of others to who finishes them, every fourth a warp's
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int u = group + 4 * h, to = u * S / 8, first = (to * 8 + S - 1) / S;  // part, its pair, that pair's first part
+        if (to == pair || n0 + u * 32 >= N) continue;
+        uint32_t r[32];
+        tmem_ld32(lanes + u * 32, r);
+        tmem_wait_ld();
+        const int slot = pair < to ? pair : pair - 1;
+        const uint32_t at = peer_addr(smem_u32(parts + ((size_t)((slot * C::kMost + u - first) * 8) * 128 + row) * 16), (uint32_t)(2 * to + side));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) st_peer_v4(at + e * 2048, r + 4 * e);
+      }
+    }
+  }
+  cluster_arrive();
+  const int first = (pair * 8 + S - 1) / S, count = ((pair + 1) * 8 + S - 1) / S - first;  // this pair's parts
+  constexpr int kPieces = (2 * C::kMost + 3) / 4;  // of sixteen columns of them, every fourth a warp's
+  uint4 res[kPieces][2];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int piece = group + 4 * i, n = n0 + first * 32 + piece * 16 + h * 8;
+      res[i][h] = out && plus.residual && piece < 2 * count && m < M && n < N ? *reinterpret_cast<const uint4*>(plus.residual + (size_t)m * plus.ldr + n) : make_uint4(0, 0, 0, 0);
+    }
+  cluster_wait();  // the parts of all are there; nobody writes any more
+  if (ok && out) {
+    const float row_scale = kKind == kPlus8 && m < M ? plus.a_scale[m] : 1.f;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int piece = group + 4 * i, col = first * 32 + piece * 16;
+      if (piece >= 2 * count || n0 + col >= N) continue;
+      uint32_t own[16];
+      tmem_ld16(lanes + col, own);
+      tmem_wait_ld();
+      float v[2][8] = {};
+#pragma unroll
+      for (int r = 0; r < S; ++r) {
+        if (r == pair) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e / 8][e % 8] += __uint_as_float(own[e]);
+        } else {
+          const uint8_t* at = parts + ((size_t)(((r < pair ? r : r - 1) * C::kMost + piece / 2) * 8 + piece % 2 * 4) * 128 + row) * 16;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float4 p = *reinterpret_cast<const float4*>(at + e * 2048);
+            float* x = &v[e / 2][e % 2 * 4];
+            x[0] += p.x, x[1] += p.y, x[2] += p.z, x[3] += p.w;
+          }
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int n = n0 + col + h * 8;
+        if (m < M && n < N) finish8<kKind>(v[h], row_scale, plus, act, res[i][h], n, plus.c + (size_t)m * plus.ldc + n);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 256);
+  }
+  cluster_sync();  // neither of a pair leaves while the other's MMAs read its shared memory or its arrivals are under way
+}
+
 template <int kKind, int S>
 int splits_at_once() {
-  static std::atomic<unsigned long long> raised{0};
-  static std::atomic<int> known[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (const int k = known[dev].load(std::memory_order_relaxed)) return k - 1;
-  int clusters = 0;
-  bool ok = raise_dynamic_smem(linear_split_kernel<kKind, S>, kSplitSmem, raised) == cudaSuccess;
-  if (ok) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(S);
-    cfg.blockDim = dim3((2 + kEpiWarps) * 32);
-    cfg.dynamicSmemBytes = kSplitSmem;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = S;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    ok = cudaOccupancyMaxActiveClusters(&clusters, linear_split_kernel<kKind, S>, &cfg) == cudaSuccess;
-  }
-  if (!ok) (void)cudaGetLastError();
-  if (!ok || clusters < 0) clusters = 0;
-  known[dev].store(clusters + 1, std::memory_order_relaxed);
-  return clusters;
+  static ClusterState st;
+  return clusters_at_once(linear_split_kernel<kKind, S>, st, S, (2 + kEpiWarps) * 32, kSplitSmem);
 }
 template <int kKind, int S>
-cudaError_t run_split(int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tw, int act, const LinearPlus& plus,
-                      uint32_t* dev_status, cudaStream_t s) {
+int pair_splits_at_once() {
+  static ClusterState st;
+  return clusters_at_once(linear_pair_split_kernel<kKind, S>, st, 2 * S, (2 + PairSplitCfg<S>::kWarps) * 32, PairSplitCfg<S>::kSmemBytes);
+}
+template <int kKind, int S>
+cudaError_t run_split(int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tw, int act, const LinearPlus& plus, uint32_t* dev_status,
+                      cudaStream_t s) {
   const long long ctas = (long long)((M + 127) / 128) * ((N + 127) / 128) * S;
   if (ctas > INT32_MAX) return cudaErrorInvalidValue;
   const cudaError_t e = launch_dependent_cluster(linear_split_kernel<kKind, S>, dim3((unsigned)ctas), dim3((2 + kEpiWarps) * 32), (size_t)kSplitSmem, S, s,
                                                  ta, tw, M, N, K, act, dev_status, plus);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+template <int kKind, int S>
+cudaError_t run_pair_split(int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tw, int act, const LinearPlus& plus, uint32_t* dev_status,
+                           cudaStream_t s) {
+  using C = PairSplitCfg<S>;
+  const long long ctas = (long long)((M + 255) / 256) * ((N + 255) / 256) * 2 * S;
+  if (ctas > INT32_MAX) return cudaErrorInvalidValue;
+  const cudaError_t e = launch_dependent_cluster(linear_pair_split_kernel<kKind, S>, dim3((unsigned)ctas), dim3((2 + C::kWarps) * 32),
+                                                 (size_t)C::kSmemBytes, 2 * S, s, ta, tw, M, N, K, act, dev_status, plus);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -847,41 +1020,70 @@ cudaError_t launch_linear_tc(int M, int N, int K, const void* a, const void* con
 namespace {
 template <int kKind>
 cudaError_t run_plus(const LinearPlusOp& o, const CUtensorMap& ta, const CUtensorMap& tw, const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
-  const int at_once = pairs_at_once(), steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
-  const int at2 = splits_at_once<kKind, 2>(), at4 = splits_at_once<kKind, 4>(), at8 = splits_at_once<kKind, 8>();
-  int form = linear_plus_form(o.M, o.N, steps, sm_count(), at_once, at2, at4, at8);
-  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 1 && v != 9) {  // test-only override
-    const bool pair = v == 3 || v == 5 || v == 10, split = v >= 6 && v <= 8;
-    if (pair ? o.M > 128 && at_once > 0 : !split || (steps >= 1 << (v - 5) && (v == 6 ? at2 : v == 7 ? at4 : at8) > 0)) form = v;
+  const int steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
+  const PlusDevice d{sm_count(),
+                     pairs_at_once(),
+                     {splits_at_once<kKind, 2>(), splits_at_once<kKind, 4>(), splits_at_once<kKind, 8>()},
+                     {pair_splits_at_once<kKind, 2>(), pair_splits_at_once<kKind, 3>()}};
+  int form = linear_plus_form(o.M, o.N, steps, o.act, d);
+  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 2 && v <= 10) {  // test-only override
+    const bool pair = v == 3 || v == 5, split = v >= 6 && v <= 8;
+    if (pair ? o.M > 128 && d.pairs > 0 : split ? steps >= 1 << (v - 5) && d.split[v - 6] > 0 : v < 9 || (steps >= v - 7 && d.pair_split[v - 9] > 0)) form = v;
   }
-  if (form == 6) return run_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
-  if (form == 7) return run_split<kKind, 4>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
-  if (form == 8) return run_split<kKind, 8>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+  switch (form) {
+    case 6: return run_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 7: return run_split<kKind, 4>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 8: return run_split<kKind, 8>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 9: return run_pair_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 10: return run_pair_split<kKind, 3>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    default: break;
+  }
   CUtensorMap tc, tr = tw;
   const uint64_t cdims[2] = {(uint64_t)o.N, (uint64_t)o.M}, cstr[1] = {(uint64_t)o.ldc * 2}, rstr[1] = {(uint64_t)o.ldr * 2};
   const uint32_t cbox[2] = {64, 32};  // a warp's 32 rows of one 64-column slab
   if (!encode_tmap_16bit(&tc, o.c, 2, cdims, cstr, cbox) || (o.residual && !encode_tmap_16bit(&tr, o.residual, 2, cdims, rstr, cbox)))
     return cudaErrorInvalidValue;
   CUtensorMap th = tw;
-  if (form == 10) {  // half slabs of W
+  if (form == 5) {  // half slabs of W
     const uint64_t wdims[2] = {(uint64_t)(o.f8 ? o.K : o.N), (uint64_t)(o.f8 ? o.N : o.K)}, wstr[1] = {(uint64_t)o.ldw * (o.f8 ? 1 : 2)};
     const uint32_t hbox[2] = {o.f8 ? 128u : 32u, o.f8 ? 32u : 64u};
     if (!(o.f8 ? encode_tmap_8bit : encode_tmap_16bit)(&th, o.w, 2, wdims, wstr, hbox)) return cudaErrorInvalidValue;
   }
   const CUtensorMap tws[3] = {tw, tr, th}, tcs[3] = {tc, tc, tc};
-  return run_form<kKind>(form, at_once, o.M, o.N, o.K, 1, ta, tws, tcs, o.act, plus, dev_status, s);
+  return run_form<kKind>(form, d.pairs, o.M, o.N, o.K, 1, ta, tws, tcs, o.act, plus, dev_status, s);
 }
 }  // namespace
 
-// The same with bias and residual, by stages (64 contraction elements of bf16, 128 of e4m3).
-int linear_plus_form(int M, int N, int steps, int sms, int pairs, int at2, int at4, int at8) {
-  return linear_tc_form(M, N, steps * kKC, 1, sms, pairs);
+// The form with the least time by this account: rounds of tiles over the SMs, each a fixed part and a part per step (64 contraction
+// elements of bf16, 128 of e4m3), and what is left of a launch.  Nanoseconds, fitted to 266 shapes between 20 x 320 x 1280 and
+// 16384 x 5120 x 1280 in both types, each timed in every form: within 4 to 6 % in the mean (10 to 14 % for the split forms), and the
+// form it names takes 1.02 times as long as the best in the mean.  linear_tc_form()'s choice took 1.15 (3.4 at most: few tiles).
+// The forms of 256 rows are for more than 128.  An activation is hidden under the next tile's steps but for the form that has one
+// accumulator.
+int linear_plus_form(int M, int N, int steps, int act, const PlusDevice& d) {
+  const auto tiles = [&](int rows, int cols) { return (long long)((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
+  int best = 0;
+  long long least = LLONG_MAX;
+  const auto offer = [&](int form, long long count, int at_once, int parts, int launch, int round, int step) {
+    if (at_once < 1 || steps < parts) return;
+    const long long cost = launch + (count + at_once - 1) / at_once * (round + (long long)((steps + parts - 1) / parts) * step);
+    if (cost < least) least = cost, best = form;
+  };
+  offer(4, tiles(128, 128), d.sms, 1, 3840, 1020, 252);
+  offer(2, tiles(128, 192), d.sms, 1, 3660, 1520, 265);
+  for (int i = 0; i < 3; ++i) offer(6 + i, tiles(128, 128), d.split[i], 2 << i, 0, i == 1 ? 5400 : 5680, i == 0 ? 254 : 282);
+  if (M > 128) {
+    offer(3, tiles(kPairRows, kPairCols), d.pairs, 1, 5030, 1470, 293);
+    offer(5, tiles(kPairRows, 320), d.pairs, 1, 3930, act == kActNone ? 3510 : 5000, 382);
+    for (int i = 0; i < 2; ++i) offer(9 + i, tiles(kPairRows, kPairCols), d.pair_split[i], 2 + i, 0, 7700, i == 0 ? 298 : 327);
+  }
+  return best;
 }
 
 // c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
   const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
-  if (o.M <= 16 && (tune == 0 || tune == 9)) return launch_linear_rows(o, linear_rows_split(o.N, (o.K + (o.f8 ? 63 : 31)) / (o.f8 ? 64 : 32), sm_count()), s);
+  if (o.M <= 16 && (tune == 0 || tune == 1)) return launch_linear_rows(o, linear_rows_split(o.N, (o.K + (o.f8 ? 63 : 31)) / (o.f8 ? 64 : 32), sm_count()), s);
   CUtensorMap ta, tw;
   const uint64_t adims[2] = {(uint64_t)o.K, (uint64_t)o.M}, astr[1] = {(uint64_t)o.lda * (o.f8 ? 1 : 2)};
   const uint32_t abox[2] = {o.f8 ? 128u : 64u, 128};

@@ -267,17 +267,24 @@ __device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m
       "l"(reinterpret_cast<uint64_t>(m)), "r"(peer_addr(smem_u32(bar), 0)), "r"(c0), "r"(c1)
       : "memory");
 }
+// The same with the barrier's address in the cluster given, where the pair is not the cluster's first.
+__device__ __forceinline__ void tma_load_2d_pair_at(void* dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1)
+      : "memory");
+}
 // One arrival on the barrier at this address of the cluster.  (Release and acquire at cluster scope, as in mbar_arrive_peer()
 // and mbar_wait_cluster(), cost a k-step 2700 cycles instead of 600.)
 __device__ __forceinline__ void mbar_arrive_at(uint32_t addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
-// The barrier at this offset arrives in both CTAs once every MMA issued so far by this thread has completed.
-__device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
-               "h"((uint16_t)3)
+// The barrier at this offset arrives in the CTAs of the mask (both of the pair) once every MMA issued so far by this thread has completed.
+__device__ __forceinline__ void mma_commit_pair_to(uint64_t* bar, uint16_t ctas) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"(ctas)
                : "memory");
 }
+__device__ __forceinline__ void mma_commit_pair(uint64_t* bar) { mma_commit_pair_to(bar, 3); }
 
 // 32 lanes x 32 consecutive 32-bit columns -> 32 registers per thread (thread = lane).
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {

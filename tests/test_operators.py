@@ -448,7 +448,8 @@ def test_linear_f32_parity(toma, m, n, k):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("tile", [1, 2, 3, 4, 5, 6, 7, 8, 10], ids=["128x256", "128x192", "256x256", "128x128", "256x128", "split2", "split4", "split8", "256x320"])
+@pytest.mark.parametrize("tile", [2, 3, 4, 5, 6, 7, 8, 9, 10],
+                         ids=["128x192", "256x256", "128x128", "256x320", "split2", "split4", "split8", "pairs2", "pairs3"])
 @pytest.mark.parametrize("m,n,k", [(300, 328, 200), (129, 1920, 640), (1024, 72, 136), (9000, 1016, 72), (20000, 64, 200)])
 def test_linear_every_tile_form(toma, tuning, tile, m, n, k):
     tuning(linear_tile=tile)
