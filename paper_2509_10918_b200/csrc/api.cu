@@ -460,7 +460,7 @@ static bool bad_ld(int ld, int cols, int multiple) { return ld < cols || ld % mu
 
 static toma_status norm_check(const NormOp& o, int esz, int y_esz, int ld_multiple, int ldy_multiple) {
   if (o.rows < 1 || o.dim < 8 || o.dim % 8) return TOMA_ERR_SHAPE;
-  if (o.dim > 16384) return TOMA_ERR_UNSUPPORTED;
+  if (o.dim > 16384 || o.rows > 1 << 30) return TOMA_ERR_UNSUPPORTED;
   if (!o.x || !o.y || (o.sum && !o.delta)) return TOMA_ERR_NULL;
   if (bad_ld(o.ldx, o.dim, ld_multiple) || (o.delta && bad_ld(o.ldd, o.dim, ld_multiple)) || (o.sum && bad_ld(o.lds, o.dim, ld_multiple)) ||
       bad_ld(o.ldy, o.dim, ldy_multiple))
@@ -497,6 +497,7 @@ toma_status toma_rms_norm_q8(int32_t rows, int32_t dim, const void* x, int32_t l
 // Every error of a projection with its epilogue that the host can see.
 static toma_status linear_plus_check(const LinearPlusOp& o, bool f32) {
   if (o.M < 1 || o.N < 1 || o.K < 1) return TOMA_ERR_SHAPE;
+  if (o.M > 1 << 30 || o.N > 1 << 24 || o.K > 1 << 24) return TOMA_ERR_UNSUPPORTED;  // what the index arithmetic is made for
   if (!o.a || !o.w || !o.c || (o.f8 && (!o.a_scale || !o.w_scale))) return TOMA_ERR_NULL;
   if (misaligned(o.a) || misaligned(o.w) || misaligned(o.c) || misaligned(o.bias) || misaligned(o.residual) || misaligned(o.w_scale) ||
       ((uintptr_t)o.a_scale & 3))
@@ -537,6 +538,7 @@ toma_status toma_linear_q8(int32_t m, int32_t n, int32_t k, const void* a, int32
 
 toma_status toma_quantise_weight(int32_t k, int32_t n, const void* w, void* q, int32_t ldq, float* scale, void* stream) {
   if (k < 8 || n < 8 || k % 8 || n % 8) return TOMA_ERR_SHAPE;
+  if (k > 1 << 24 || n > 1 << 24) return TOMA_ERR_UNSUPPORTED;
   if (!w || !q || !scale) return TOMA_ERR_NULL;
   if (misaligned(w) || misaligned(q) || misaligned(scale) || bad_ld(ldq, k, 16)) return TOMA_ERR_SHAPE;
   const Rows wr = rows_of(w, k, n, n, 2), qr = rows_of(q, n, k, ldq, 1), sr = rows_of(scale, 1, n, n, 4);

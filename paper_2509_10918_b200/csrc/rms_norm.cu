@@ -24,125 +24,182 @@ __device__ __forceinline__ float sum_row(float v, float* red, int t) {
   }
   return v;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {  // a number that is none stays one
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 template <int kLanes>
-__device__ __forceinline__ uint32_t max_row(uint32_t v, uint32_t* red, int t) {
+__device__ __forceinline__ float max_row(float v, float* red, int t) {
 #pragma unroll
-  for (int o = kLanes < 32 ? kLanes / 2 : 16; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  for (int o = kLanes < 32 ? kLanes / 2 : 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
   if constexpr (kLanes > 32) {
     if ((t & 31) == 0) red[t >> 5] = v;
     __syncthreads();
-    v = 0;
+    v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kLanes / 32; ++w) v = max(v, red[w]);
+    for (int w = 0; w < kLanes / 32; ++w) v = max_nan(v, red[w]);
   }
   return v;
 }
 
-// kLanes threads per row, kVec packets of 8 elements in each.
-template <typename T, bool kQ8, int kLanes, int kVec>
-__global__ void __launch_bounds__(kLanes < 256 ? 256 : kLanes) rms_norm_kernel(const NormOp o) {
+// Blocks of an SM at once: what the registers of a thread allow (packets of x, delta and weight as they lie in memory, h as floats).
+template <typename T, bool kAdd, int kLanes, int kVec>
+constexpr int kNormCtas = kLanes > 256 ? (kVec * sizeof(T) <= 4 ? 2 : 1) : kVec * (sizeof(T) == 2 ? (kAdd ? 20 : 16) : (kAdd ? 32 : 24)) + 30 <= 64 ? 4 : kVec * (sizeof(T) == 2 ? (kAdd ? 20 : 16) : (kAdd ? 32 : 24)) + 30 <= 84 ? 3 : kVec * (sizeof(T) == 2 ? (kAdd ? 20 : 16) : (kAdd ? 32 : 24)) + 30 <= 128 ? 2 : 1;
+
+// Packets of eight elements as they lie in memory.
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> { uint4 q; };
+template <> struct Raw<float> { float4 q[2]; };
+__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, Raw<__nv_bfloat16>& r) { r.q = *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void load_raw(const float* p, Raw<float>& r) {
+  r.q[0] = reinterpret_cast<const float4*>(p)[0];
+  r.q[1] = reinterpret_cast<const float4*>(p)[1];
+}
+__device__ __forceinline__ void widen(const Raw<__nv_bfloat16>& r, float (&v)[8]) {
+  const uint32_t w[4] = {r.q.x, r.q.y, r.q.z, r.q.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[2 * e] = __uint_as_float(w[e] << 16);
+    v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void widen(const Raw<float>& r, float (&v)[8]) {
+  v[0] = r.q[0].x, v[1] = r.q[0].y, v[2] = r.q[0].z, v[3] = r.q[0].w, v[4] = r.q[1].x, v[5] = r.q[1].y, v[6] = r.q[1].z, v[7] = r.q[1].w;
+}
+__device__ __forceinline__ float max3_abs(float top, float a, float b) {  // a number that is none stays one
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(top), "f"(fabsf(a)), "f"(fabsf(b)));
+  return d;
+}
+
+// kLanes threads per row, kVec packets of 8 elements in each.  A row's threads go on to further rows, the next one's elements on
+// their way while this one's are worked on; the weight stays in registers.
+template <typename T, bool kQ8, bool kAdd, int kLanes, int kVec>
+__global__ void __launch_bounds__(kLanes < 256 ? 256 : kLanes, kNormCtas<T, kAdd, kLanes, kVec>) rms_norm_kernel(const NormOp o) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
-  __shared__ float red_s[kRows][kLanes / 32];
-  __shared__ uint32_t red_m[kRows][kLanes / 32];
+  __shared__ float red_s[2][kRows][(kLanes + 31) / 32], red_m[2][kRows][(kLanes + 31) / 32];
   const int group = threadIdx.x / kLanes, t = threadIdx.x % kLanes;
-  const int row = blockIdx.x * kRows + group;
-  const bool live = row < o.rows;
   tc::dependency_wait();  // launched with programmatic stream serialisation
   if (threadIdx.x == 0) tc::release_dependents();
-  const T* x = (const T*)o.x + (size_t)row * o.ldx;
-  const T* delta = (const T*)o.delta + (size_t)row * o.ldd;
-  const T* weight = (const T*)o.weight;
-  float h[kVec][8];
+  const bool weighted = o.weight != nullptr;
+  const float inv_dim = 1.f / (float)o.dim;
+  bool in[kVec];
+  Raw<T> w[kVec], x[kVec], d[kAdd ? kVec : 1];
 #pragma unroll
   for (int v = 0; v < kVec; ++v) {
-    const int e = (v * kLanes + t) * 8;
-    if (live && e < o.dim) load8(x + e, h[v]);
-    else
-#pragma unroll
-      for (int u = 0; u < 8; ++u) h[v][u] = 0.f;
+    in[v] = (v * kLanes + t) * 8 < o.dim;
+    w[v] = x[v] = Raw<T>{};
+    if constexpr (kAdd) d[v] = Raw<T>{};
+    if (in[v] && weighted) load_raw((const T*)o.weight + (v * kLanes + t) * 8, w[v]);
   }
-  if (o.delta) {
+  const auto fetch = [&](int row) {
+#pragma unroll
+    for (int v = 0; v < kVec; ++v)
+      if (in[v]) {
+        load_raw((const T*)o.x + (size_t)row * o.ldx + (v * kLanes + t) * 8, x[v]);
+        if constexpr (kAdd) load_raw((const T*)o.delta + (size_t)row * o.ldd + (v * kLanes + t) * 8, d[v]);
+      }
+  };
+  // (all threads of a block take the same number of turns: there are barriers in them where a row is several warps')
+  int row = blockIdx.x * kRows + group;
+  if (row < o.rows) fetch(row);
+  for (int base = blockIdx.x * kRows, turn = 0; base < o.rows; base += gridDim.x * kRows, ++turn) {
+    const bool live = row < o.rows;
+    float h[kVec][8];
 #pragma unroll
     for (int v = 0; v < kVec; ++v) {
-      const int e = (v * kLanes + t) * 8;
-      if (live && e < o.dim) {
-        float d[8];
-        load8(delta + e, d);
+      widen(x[v], h[v]);
+      if constexpr (kAdd) {
+        float e[8];
+        widen(d[v], e);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          T r;
-          from_f32(r, h[v][u] + d[u]);
-          h[v][u] = to_f32(r);
+        for (int u = 0; u < 8; ++u) h[v][u] += e[u];
+        if constexpr (sizeof(T) == 2) {  // rounded to the stream's type
+          __align__(16) __nv_bfloat162 q[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(h[v][2 * u], h[v][2 * u + 1]);
+          const Raw<T> r{*reinterpret_cast<const uint4*>(q)};
+          if (o.sum && live && in[v]) *reinterpret_cast<uint4*>((T*)o.sum + (size_t)row * o.lds + (v * kLanes + t) * 8) = r.q;
+          widen(r, h[v]);
+        } else {
+          if (o.sum && live && in[v]) store8((T*)o.sum + (size_t)row * o.lds + (v * kLanes + t) * 8, h[v]);
         }
-        if (o.sum) store8((T*)o.sum + (size_t)row * o.lds + e, h[v]);
       }
     }
-  }
-  float ss = 0.f;
+    const int next = row + (int)gridDim.x * kRows;
+    if (next < o.rows) fetch(next);
+    uint64_t ss2 = 0;
 #pragma unroll
-  for (int v = 0; v < kVec; ++v)
+    for (int v = 0; v < kVec; ++v)
 #pragma unroll
-    for (int u = 0; u < 8; ++u) ss = fmaf(h[v][u], h[v][u], ss);
-  ss = sum_row<kLanes>(ss, red_s[group], t);
-  const float r = 1.f / sqrtf(ss / (float)o.dim + o.eps);
-  if constexpr (!kQ8) {
-#pragma unroll
-    for (int v = 0; v < kVec; ++v) {
-      const int e = (v * kLanes + t) * 8;
-      if (live && e < o.dim) {
-        float w[8];
-        if (weight) load8(weight + e, w);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) w[u] = weight ? h[v][u] * r * w[u] : h[v][u] * r;
-        store8((T*)o.y + (size_t)row * o.ldy + e, w);
+      for (int u = 0; u < 8; u += 2) {
+        const uint64_t p = tc::pack2(h[v][u], h[v][u + 1]);
+        ss2 = tc::fma2(p, p, ss2);
       }
-    }
-  } else {
-    uint32_t top_bits = 0;
+    float s0, s1;
+    tc::unpack2(ss2, s0, s1);
+    const float ss = sum_row<kLanes>(s0 + s1, red_s[turn & 1][group], t);
+    // (what is rounded to 8 or 16 bits or multiplies such: within 2 units of the last place is enough)
+    const float r = sizeof(T) == 4 ? 1.f / sqrtf(ss / (float)o.dim + o.eps) : rsqrtf(fmaf(ss, inv_dim, o.eps));
+    if constexpr (!kQ8) {
 #pragma unroll
-    for (int v = 0; v < kVec; ++v) {
-      const int e = (v * kLanes + t) * 8;
-      if (weight && live && e < o.dim) {
-        float w[8];
-        load8(weight + e, w);
+      for (int v = 0; v < kVec; ++v) {
+        float f[8];
+        widen(w[v], f);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) h[v][u] *= w[u];
+        for (int u = 0; u < 8; ++u) f[u] = weighted ? h[v][u] * r * f[u] : h[v][u] * r;
+        if (live && in[v]) store8((T*)o.y + (size_t)row * o.ldy + (v * kLanes + t) * 8, f);
       }
+    } else {
+      float top = 0.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) top_bits = max(top_bits, abs_bits(h[v][u]));
-    }
-    top_bits = max_row<kLanes>(top_bits, red_m[group], t);
-    const float top = __uint_as_float(top_bits);
-    // a row with an infinity or none-number in it has none-numbers in its place and as its scale
-    const bool none = top_bits >= 0x7F800000u, zero = top < kE4m3Tiny;
-    const float f = none ? __uint_as_float(0x7FC00000u) : zero ? 0.f : kE4m3Max / top;
+      for (int v = 0; v < kVec; ++v) {
+        if (weighted) {
+          float f[8];
+          widen(w[v], f);
 #pragma unroll
-    for (int v = 0; v < kVec; ++v) {
-      const int e = (v * kLanes + t) * 8;
-      if (live && e < o.dim) *reinterpret_cast<uint2*>((uint8_t*)o.y + (size_t)row * o.ldy + e) = e4m3_packet(h[v], f, top);
+          for (int u = 0; u < 8; u += 2) tc::unpack2(tc::mul2(tc::pack2(h[v][u], h[v][u + 1]), tc::pack2(f[u], f[u + 1])), h[v][u], h[v][u + 1]);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; u += 2) top = max3_abs(top, h[v][u], h[v][u + 1]);
+      }
+      top = max_row<kLanes>(top, red_m[turn & 1][group], t);
+      const E4m3Row q8(top);
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) {
+        const uint2 q = q8.packet(h[v]);
+        if (live && in[v]) *reinterpret_cast<uint2*>((uint8_t*)o.y + (size_t)row * o.ldy + (v * kLanes + t) * 8) = q;
+      }
+      if (live && t == 0) o.scale[row] = r * q8.scale();
     }
-    if (live && t == 0) o.scale[row] = none ? __uint_as_float(0x7FC00000u) : zero ? 0.f : r * top * (1.f / kE4m3Max);
+    row = next;
   }
 }
 
-template <typename T, bool kQ8, int kLanes, int kVec>
+template <typename T, bool kQ8, bool kAdd, int kLanes, int kVec>
 cudaError_t run_norm(const NormOp& o, cudaStream_t s) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
+  const int blocks = (o.rows + kRows - 1) / kRows, most = sm_count() * kNormCtas<T, kAdd, kLanes, kVec>;
   count_launch();
-  return launch_dependent(rms_norm_kernel<T, kQ8, kLanes, kVec>, dim3((o.rows + kRows - 1) / kRows), dim3(kRows * kLanes), 0, s, o);
+  return launch_dependent(rms_norm_kernel<T, kQ8, kAdd, kLanes, kVec>, dim3(blocks < most ? blocks : most), dim3(kRows * kLanes), 0, s, o);
 }
 
-template <typename T, bool kQ8>
+template <typename T, bool kQ8, bool kAdd>
 cudaError_t norm_form(const NormOp& o, cudaStream_t s) {
   const int packets = (o.dim + 7) / 8;
-  if (packets <= 32) return run_norm<T, kQ8, 32, 1>(o, s);
-  if (packets <= 64) return run_norm<T, kQ8, 32, 2>(o, s);
-  if (packets <= 96) return run_norm<T, kQ8, 32, 3>(o, s);
-  if (packets <= 128) return run_norm<T, kQ8, 32, 4>(o, s);
-  if (packets <= 256) return run_norm<T, kQ8, 128, 2>(o, s);
-  if (packets <= 512) return run_norm<T, kQ8, 128, 4>(o, s);
-  if (packets <= 1024) return run_norm<T, kQ8, 512, 2>(o, s);
-  return run_norm<T, kQ8, 512, 4>(o, s);
+  if (packets <= 8) return run_norm<T, kQ8, kAdd, 8, 1>(o, s);
+  if (packets <= 16) return run_norm<T, kQ8, kAdd, 16, 1>(o, s);
+  if (packets <= 32) return run_norm<T, kQ8, kAdd, 32, 1>(o, s);
+  if (packets <= 64) return run_norm<T, kQ8, kAdd, 32, 2>(o, s);
+  if (packets <= 96) return run_norm<T, kQ8, kAdd, 32, 3>(o, s);
+  if (packets <= 128) return run_norm<T, kQ8, kAdd, 32, 4>(o, s);
+  if (packets <= 160) return run_norm<T, kQ8, kAdd, 32, 5>(o, s);
+  if (packets <= 256) return run_norm<T, kQ8, kAdd, 128, 2>(o, s);
+  if (packets <= 384) return run_norm<T, kQ8, kAdd, 128, 3>(o, s);
+  if (packets <= 512) return run_norm<T, kQ8, kAdd, 128, 4>(o, s);
+  if (packets <= 1024) return run_norm<T, kQ8, kAdd, 512, 2>(o, s);
+  return run_norm<T, kQ8, kAdd, 512, 4>(o, s);
 }
 
 // A CTA's 32 columns of w [K][N]: their maxima, then the columns as rows of q.  (Once per model: two reads, the second from L2.)
@@ -169,9 +226,8 @@ __global__ void __launch_bounds__(256) quantise_weight_kernel(int K, int N, cons
   if (t < 32) {
     uint32_t m = 0;
     for (int l = 0; l < 64; ++l) m = max(m, red[l][t]);
-    const float f = __uint_as_float(m);
-    top_of[t] = f;
-    if (n0 + t < N) scale[n0 + t] = m >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : f < kE4m3Tiny ? 0.f : f * (1.f / kE4m3Max);
+    top_of[t] = __uint_as_float(m);
+    if (n0 + t < N) scale[n0 + t] = E4m3Row(top_of[t]).scale();
   }
   for (int k0 = 0; k0 < K; k0 += kQwRows) {
     __syncthreads();
@@ -188,8 +244,7 @@ __global__ void __launch_bounds__(256) quantise_weight_kernel(int K, int N, cons
       float p[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) p[u] = tile[k + u][col];
-      const float m = top_of[col], f = abs_bits(m) >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : m < kE4m3Tiny ? 0.f : kE4m3Max / m;
-      *reinterpret_cast<uint2*>(q + (size_t)(n0 + col) * ldq + k0 + k) = e4m3_packet(p, f, m);
+      *reinterpret_cast<uint2*>(q + (size_t)(n0 + col) * ldq + k0 + k) = E4m3Row(top_of[col]).packet(p);
     }
   }
 }
@@ -197,7 +252,10 @@ __global__ void __launch_bounds__(256) quantise_weight_kernel(int K, int N, cons
 }  // namespace
 
 cudaError_t launch_rms_norm(const NormOp& o, cudaStream_t s) {
-  const cudaError_t e = o.scale ? norm_form<__nv_bfloat16, true>(o, s) : o.f32 ? norm_form<float, false>(o, s) : norm_form<__nv_bfloat16, false>(o, s);
+  const bool add = o.delta != nullptr;
+  const cudaError_t e = o.scale ? (add ? norm_form<__nv_bfloat16, true, true>(o, s) : norm_form<__nv_bfloat16, true, false>(o, s))
+                        : o.f32 ? (add ? norm_form<float, false, true>(o, s) : norm_form<float, false, false>(o, s))
+                                : (add ? norm_form<__nv_bfloat16, false, true>(o, s) : norm_form<__nv_bfloat16, false, false>(o, s));
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
