@@ -517,7 +517,8 @@ static toma_status linear_plus_check(const LinearPlusOp& o, bool f32) {
 }
 
 static cudaError_t do_linear_plus(const LinearPlusOp& o, bool f32, uint32_t* dev_status, cudaStream_t s) {
-  return f32 ? launch_linear_plus_simt(o, s) : launch_linear_plus_tc(o, dev_status, s);
+  if (!f32) return launch_linear_plus_tc(o, dev_status, s);
+  return linear_f32_tc_ok(o) ? launch_linear_f32_tc(o, dev_status, s) : launch_linear_plus_simt(o, s);
 }
 
 toma_status toma_linear_act(int32_t m, int32_t n, int32_t k, int32_t dtype, const void* a, int32_t lda, const void* w, const void* bias, int32_t act,

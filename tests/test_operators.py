@@ -447,6 +447,53 @@ def test_linear_f32_parity(toma, m, n, k):
     run_linear(toma, m, n, k, F32, False, "silu", False, pad=5, seed=1)
 
 
+F32_SHAPES = [(17, 4, 4), (20, 640, 2560), (128, 64, 64), (130, 200, 132), (300, 72, 1000), (515, 1284, 68), (1003, 2560, 640), (2048, 320, 2560), (64, 64, 20000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", [0, 1, 2, 3, 4, 5, 6], ids=["chosen", "128", "64", "128split2", "128split4", "64split2", "64split4"])
+def test_linear_f32_on_the_tensor_cores(toma, tuning, form):
+    """Floats as sums of three bf16 numbers: the bound of a sum in fp32, the length of the longest among them."""
+    tuning(linear_tile=form)
+    for m, n, k in F32_SHAPES:
+        run_linear(toma, m, n, k, F32, True, "gelu_tanh", True, pad=8)
+        run_linear(toma, m, n, k, F32, False, "none", False, seed=1)
+
+
+@pytest.mark.gpu
+def test_linear_f32_error_is_that_of_fp32_sums(toma):
+    """On the tensor cores and not: the root of the mean square error against 64 bits, in units of 2^-24 of the results' root mean
+    square.  A sum of k products of random signs has an error of about sqrt(k) / 3 of them at most where it is rounded after each."""
+    for m, n, k in ((512, 256, 640), (512, 256, 4096), (512, 257, 640)):
+        g = generator(m, n, k)
+        a, w, c = rand(g, m, k), rand(g, k, n), torch.empty(m, n, device="cuda")
+        toma.toma_linear_act(a, w, c)
+        want = a.double() @ w.double()
+        off = float(((c.double() - want).square().mean() / want.square().mean()).sqrt()) * 2 ** 24
+        print(f"f32 {m} x {n} x {k}: {off:.2f} units of 2^-24")
+        assert off <= math.sqrt(k)
+
+
+@pytest.mark.gpu
+def test_linear_f32_with_infinities_and_none_numbers(toma):
+    """Rows and columns with infinities have the infinities that the sums have, rows with a none-number have nothing else."""
+    g = generator(9)
+    a, w = rand(g, 300, 260), rand(g, 260, 136)
+    a[3, 7], a[5, 100], a[5, 200], a[290, 259], a[8, 0] = float("inf"), float("-inf"), float("inf"), float("nan"), 3.4e38
+    w[11, 50], w[0, 60] = float("inf"), 1e30
+    c = torch.empty(300, 136, device="cuda")
+    toma.toma_linear_act(a, w, c)
+    torch.cuda.synchronize()
+    with_inf = a.double() @ w.double()
+    want = torch.where(with_inf.abs() > torch.finfo(F32).max, torch.sign(with_inf) * float("inf"), with_inf)
+    assert torch.equal(torch.isnan(c), torch.isnan(want)) and torch.isnan(c[290]).all()
+    assert torch.equal(torch.isinf(c), torch.isinf(want)) and torch.isinf(c[3]).any() and torch.isinf(c[:, 50]).any()
+    assert torch.equal(c[torch.isinf(c)].double(), want[torch.isinf(want)])
+    fine = torch.isfinite(want)
+    tol = (a.double().abs().nan_to_num(0, 0, 0) @ w.double().abs().nan_to_num(0, 0, 0)) * 268 * 2.0 ** -23 + want.abs().nan_to_num(0, 0, 0) * 2.0 ** -23
+    assert bool(((c.double() - want).abs() <= tol)[fine].all())
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("tile", [2, 3, 4, 5, 6, 7, 8, 9, 10],
                          ids=["128x192", "256x256", "128x128", "256x320", "split2", "split4", "split8", "pairs2", "pairs3"])
