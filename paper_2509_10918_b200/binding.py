@@ -338,7 +338,10 @@ def toma_mlp(rows, dim, hidden, dtype, x, w1, w2, out, ws, dev_status=None):
 # ---- between the blocks ----
 # Tensors are checked here (type, shape, device); strides, sizes and overlaps by the library.
 
-_LD_UNIT = {torch.bfloat16: 8, torch.float32: 4, torch.float8_e4m3fn: 16}
+# These calls take a few microseconds of a host's time, most of it spent on looking at tensors: each property is asked for once.
+
+_BF16, _F32, _E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+_LD_UNIT = {_BF16: 8, _F32: 4, _E4M3: 16}
 
 
 def _refuse(t, name, dtype, shape, device):
@@ -364,16 +367,8 @@ def _rows(t, name, dtype, shape, device):
     return t.data_ptr(), ld
 
 
-def _vec(t, name, dtype, n, device):
-    """Data pointer of a contiguous vector of n elements; None for None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
-        _refuse(t, name, dtype, (n,), device)
-    return t.data_ptr()
-
-
 def _dense(t, name, dtype, shape, device):
+    """Data pointer of a contiguous tensor; None for None."""
     if t is None:
         return None
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
@@ -381,90 +376,95 @@ def _dense(t, name, dtype, shape, device):
     return t.data_ptr()
 
 
-def _matrix(t, name):
-    if t.dim() != 2:
-        raise ValueError(f"{name}: expected a matrix, got {list(t.shape)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: must live on a CUDA device (no CPU path exists)")
-    return t.shape
+def _shape2(t, name):
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name}: expected a matrix, got {list(shape)}")
+    return shape
 
 
-def _float_code(t, name) -> int:
-    if t.dtype == torch.bfloat16:
+def _float_code(dtype, name) -> int:
+    if dtype is _BF16:
         return TOMA_BF16
-    if t.dtype == torch.float32:
+    if dtype is _F32:
         return TOMA_F32
-    raise ValueError(f"{name}: expected bfloat16 or float32, got {t.dtype}")
+    raise ValueError(f"{name}: expected bfloat16 or float32, got {dtype}")
 
 
 def _current_device() -> int:
-    return torch.cuda.current_device() if _device is None else _device()
+    try:
+        return torch.cuda.current_device() if _device is None else _device()
+    except RuntimeError as e:
+        raise ValueError("tensors must live on a CUDA device (no CPU path exists)") from e
 
 
 def _act(act) -> int:
-    return ACTIVATIONS.get(act, -1) if isinstance(act, str) else int(act)
+    code = ACTIVATIONS.get(act)
+    return code if code is not None else act if isinstance(act, int) else -1
 
 
 def toma_rms_norm(x, weight, y, eps=1e-6, delta=None, sum_out=None):
     """y = rms_norm(x + delta) * weight, and the sum into sum_out: [rows, dim] tensors (rows may be strided) of one type, bf16
     or fp32.  weight [dim] or None; delta and sum_out or None.  sum_out and y may be x or delta themselves."""
-    shape = rows, dim = _matrix(x, "x")
-    code, dt, dev = _float_code(x, "x"), x.dtype, _current_device()
+    shape = rows, dim = _shape2(x, "x")
+    dt, dev = x.dtype, _current_device()
+    code = _float_code(dt, "x")
     px, ldx = _rows(x, "x", dt, shape, dev)
     pd, ldd = _rows(delta, "delta", dt, shape, dev)
     ps, lds = _rows(sum_out, "sum_out", dt, shape, dev)
     py, ldy = _rows(y, "y", dt, shape, dev)
-    _check(lib.toma_rms_norm(rows, dim, code, px, ldx, pd, ldd, _vec(weight, "weight", dt, dim, dev), eps, ps, lds, py, ldy, _stream()),
+    _check(lib.toma_rms_norm(rows, dim, code, px, ldx, pd, ldd, _dense(weight, "weight", dt, (dim,), dev), eps, ps, lds, py, ldy, _stream()),
            "toma_rms_norm")
 
 
 def toma_rms_norm_q8(x, weight, q, scale, eps=1e-6, delta=None, sum_out=None):
     """toma_rms_norm of bf16 rows with an 8-bit result: q [rows, dim] float8_e4m3fn (row stride a multiple of 16), scale [rows]
     fp32, y ~ q * scale[:, None]."""
-    shape = rows, dim = _matrix(x, "x")
-    dt, dev = torch.bfloat16, _current_device()
+    shape = rows, dim = _shape2(x, "x")
+    dt, dev = _BF16, _current_device()
     px, ldx = _rows(x, "x", dt, shape, dev)
     pd, ldd = _rows(delta, "delta", dt, shape, dev)
     ps, lds = _rows(sum_out, "sum_out", dt, shape, dev)
-    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, shape, dev)
-    _check(lib.toma_rms_norm_q8(rows, dim, px, ldx, pd, ldd, _vec(weight, "weight", dt, dim, dev), eps, ps, lds, pq, ldq,
-                                _vec(scale, "scale", torch.float32, rows, dev), _stream()), "toma_rms_norm_q8")
+    pq, ldq = _rows(q, "q", _E4M3, shape, dev)
+    _check(lib.toma_rms_norm_q8(rows, dim, px, ldx, pd, ldd, _dense(weight, "weight", dt, (dim,), dev), eps, ps, lds, pq, ldq,
+                                _dense(scale, "scale", _F32, (rows,), dev), _stream()), "toma_rms_norm_q8")
 
 
 def toma_linear_act(a, w, c, bias=None, act="none", residual=None, dev_status=None):
     """c = act(a @ w + bias) + residual: a [m, k], w [k, n], c and residual [m, n], bias [n], all bf16 or all fp32; rows of a, c
     and residual may be strided, c may be residual.  act: "none", "gelu", "gelu_tanh" or "silu"."""
-    m, k = _matrix(a, "a")
-    n = _matrix(w, "w")[1]
-    code, dt, dev = _float_code(a, "a"), a.dtype, _current_device()
-    pa, lda = _rows(a, "a", dt, (m, k), dev)
+    shape = m, k = _shape2(a, "a")
+    n = _shape2(w, "w")[1]
+    dt, dev = a.dtype, _current_device()
+    code = _float_code(dt, "a")
+    pa, lda = _rows(a, "a", dt, shape, dev)
     pr, ldr = _rows(residual, "residual", dt, (m, n), dev)
     pc, ldc = _rows(c, "c", dt, (m, n), dev)
-    _check(lib.toma_linear_act(m, n, k, code, pa, lda, _dense(w, "w", dt, (k, n), dev), _vec(bias, "bias", dt, n, dev), _act(act), pr, ldr, pc, ldc,
+    _check(lib.toma_linear_act(m, n, k, code, pa, lda, _dense(w, "w", dt, (k, n), dev), _dense(bias, "bias", dt, (n,), dev), _act(act), pr, ldr, pc, ldc,
                                _ptr(dev_status), _stream()), "toma_linear_act")
 
 
 def toma_linear_q8(a, a_scale, w, w_scale, c, bias=None, act="none", residual=None, dev_status=None):
     """c = act((a @ w.T) * a_scale[:, None] * w_scale + bias) + residual: a [m, k] and w [n, k] float8_e4m3fn (row strides
     multiples of 16), scales fp32; c, bias and residual bf16."""
-    m, k = _matrix(a, "a")
-    n = _matrix(w, "w")[0]
-    f8, dt, dev = torch.float8_e4m3fn, torch.bfloat16, _current_device()
-    pa, lda = _rows(a, "a", f8, (m, k), dev)
+    shape = m, k = _shape2(a, "a")
+    n = _shape2(w, "w")[0]
+    f8, dt, dev = _E4M3, _BF16, _current_device()
+    pa, lda = _rows(a, "a", f8, shape, dev)
     pw, ldw = _rows(w, "w", f8, (n, k), dev)
     pr, ldr = _rows(residual, "residual", dt, (m, n), dev)
     pc, ldc = _rows(c, "c", dt, (m, n), dev)
-    _check(lib.toma_linear_q8(m, n, k, pa, lda, _vec(a_scale, "a_scale", torch.float32, m, dev), pw, ldw,
-                              _vec(w_scale, "w_scale", torch.float32, n, dev), _vec(bias, "bias", dt, n, dev), _act(act), pr, ldr, pc, ldc,
+    _check(lib.toma_linear_q8(m, n, k, pa, lda, _dense(a_scale, "a_scale", _F32, (m,), dev), pw, ldw,
+                              _dense(w_scale, "w_scale", _F32, (n,), dev), _dense(bias, "bias", dt, (n,), dev), _act(act), pr, ldr, pc, ldc,
                               _ptr(dev_status), _stream()), "toma_linear_q8")
 
 
 def toma_quantise_weight(w, q, scale):
     """w [k, n] bf16 -> q [n, k] float8_e4m3fn and scale [n] fp32 for toma_linear_q8 (once per weight)."""
-    k, n = _matrix(w, "w")
+    k, n = _shape2(w, "w")
     dev = _current_device()
-    pq, ldq = _rows(q, "q", torch.float8_e4m3fn, (n, k), dev)
-    _check(lib.toma_quantise_weight(k, n, _dense(w, "w", torch.bfloat16, (k, n), dev), pq, ldq, _vec(scale, "scale", torch.float32, n, dev), _stream()),
+    pq, ldq = _rows(q, "q", _E4M3, (n, k), dev)
+    _check(lib.toma_quantise_weight(k, n, _dense(w, "w", _BF16, (k, n), dev), pq, ldq, _dense(scale, "scale", _F32, (n,), dev), _stream()),
            "toma_quantise_weight")
 
 
@@ -475,12 +475,15 @@ def toma_mlp_layer_workspace_bytes(rows, dim, hidden, dtype) -> int:
 def toma_mlp_layer(x, norm_weight, w1, b1, w2, b2, out, ws, act="gelu", eps=1e-6, delta=None, dev_status=None):
     """out = s + act(rms_norm(s) * norm_weight @ w1 + b1) @ w2 + b2 with s = x + delta: x, delta and out [rows, dim] contiguous,
     w1 [dim, hidden], w2 [hidden, dim]; norm_weight, b1, b2 and delta or None; out may be x or delta."""
-    rows, dim = _matrix(x, "x")
-    hidden = _matrix(w1, "w1")[1]
-    code, dt, dev = _float_code(x, "x"), x.dtype, _current_device()
+    rows, dim = _shape2(x, "x")
+    hidden = _shape2(w1, "w1")[1]
+    dt, dev = x.dtype, _current_device()
+    code = _float_code(dt, "x")
+    if ws.get_device() != dev:
+        raise ValueError("ws: must live on the current CUDA device")
     _check(lib.toma_mlp_layer(rows, dim, hidden, code, _dense(x, "x", dt, (rows, dim), dev), _dense(delta, "delta", dt, (rows, dim), dev),
-                              _vec(norm_weight, "norm_weight", dt, dim, dev), eps, _dense(w1, "w1", dt, (dim, hidden), dev),
-                              _vec(b1, "b1", dt, hidden, dev), _act(act), _dense(w2, "w2", dt, (hidden, dim), dev), _vec(b2, "b2", dt, dim, dev),
+                              _dense(norm_weight, "norm_weight", dt, (dim,), dev), eps, _dense(w1, "w1", dt, (dim, hidden), dev),
+                              _dense(b1, "b1", dt, (hidden,), dev), _act(act), _dense(w2, "w2", dt, (hidden, dim), dev), _dense(b2, "b2", dt, (dim,), dev),
                               _dense(out, "out", dt, (rows, dim), dev), _ptr(ws), ws.numel() * ws.element_size(), _ptr(dev_status), _stream()),
            "toma_mlp_layer")
 

@@ -76,6 +76,12 @@ __device__ __forceinline__ void by_sigmoid2(uint32_t& v0, uint32_t& v1) {
   v0 = __float_as_uint(y0);
   v1 = __float_as_uint(y1);
 }
+// To full precision: fp32 mode is what bf16 runs are checked against.
+__device__ __forceinline__ float activate_f32(float x, int act) {
+  if (act == kActNone) return x;
+  if (act == kActGelu) return 0.5f * x * erfcf(-0.70710678118654752f * x);
+  return x / (1.f + expf(-(act == kActSilu ? x : x * fmaf(0.0713548162f, x * x, 1.59576912f))));
+}
 // r[e] += the eight bf16 of a packet.
 __device__ __forceinline__ void add_packet(uint32_t* r, const uint4& b) {
   const uint32_t bb[4] = {b.x, b.y, b.z, b.w};

@@ -3,18 +3,19 @@
 // A float is the sum of three bf16 numbers, exactly: x = x0 + x1 + x2 with x0 = bf16(x), x1 = bf16(x - x0), x2 = x - x0 - x1 (8 bits
 // each of the 24).  Of the nine products of two such sums the three smallest are below 2^-25 of the whole, the other six are
 // multiplied by tcgen05, whose products are exact and whose sums are in fp32.  A long chain of such sums is not as exact as one of
-// fused multiply-adds (they are cut off, not rounded), so a chain ends with its stage of 64 contraction elements, the small
-// products first, and the stages' sums are added up by the threads, rounded: 1003 x 2560 x 640 is TODO off 64 bits, the FFMA form
-// 5.1e-7.  Six bf16 products run at some 375 TFLOP/s, FFMA at 75.
+// fused multiply-adds (they are cut off, not rounded), so a chain ends after 128 contraction elements, the five small products have one
+// of their own, and the chains' sums are added up by the threads, rounded: 512 x 256 x 640 is 1.6 units of 2^-24 off 64 bits
+// (root mean square), 7.6 on FFMA.  Six bf16 products run at some 375 TFLOP/s, FFMA at 75.
 //
-// A CTA has a tile of 128 x 128 or 128 x 64.  Sixteen warps take a stage's floats from global memory (the next stage's are on their way in
-// registers meanwhile), cut them into three planes in shared memory (two stages) and add up the sums of the stage before, 32
-// or 16 columns of a row a thread; a seventeenth issues the MMAs.  Where there are few tiles a cluster of 2, 4 or 8 CTAs splits the
-// contraction and exchanges its parts through distributed shared memory.
+// A CTA has a tile of 128 x 128 or 128 x 64.  Sixteen warps take the floats from global memory, two stages of 32 contraction elements ahead
+// in registers, cut them into three planes each in shared memory (four stages) and add up the chains' sums, 32 or 16 columns
+// of a row a thread; a seventeenth issues the MMAs.  Where there are few tiles a cluster of 2 or 4 CTAs splits the contraction
+// and exchanges its parts through distributed shared memory.
 #include <climits>
 
 #include "clusters.cuh"
 #include "common.cuh"
+#include "linear_epilogue.cuh"
 #include "tc.cuh"
 
 namespace toma {
@@ -23,17 +24,20 @@ using namespace tc;
 
 namespace {
 
-constexpr int kStep = 64;                     // contraction elements of a stage
-constexpr int kPlaneA = 128 * 128, kSlab = kStep * 128;
-constexpr int kWarps = 16;                    // that cut and add
-template <int NT> constexpr int kStageBytes = 3 * (kPlaneA + NT / 64 * kSlab);
-template <int NT> constexpr int kSmem = 1024 + 2 * kStageBytes<NT> + 256;
+constexpr int kWarps = 16;                       // that cut and add
+constexpr int kStep = 32, kSlots = 4, kChunk = 4;  // contraction elements of a stage, stages in shared memory, stages of a chain
+constexpr int kPlaneA = 128 * kStep * 2, kSlab = kStep * 128;  // rows of 64 bytes of a; 64 columns of w
+template <int NT> constexpr int kPlaneW = NT / 64 * kSlab;
+template <int NT> constexpr int kStageBytes = 3 * (kPlaneA + kPlaneW<NT>);
+template <int NT> constexpr int kSmem = 1024 + kSlots * kStageBytes<NT> + 256;
 
 struct F32Bars {
-  uint64_t full[2], done[2], taken[2];  // planes are there; products are through; sums have been taken
+  uint64_t full[kSlots], empty[kSlots];  // the planes are there; have been multiplied
+  uint64_t done[2], taken[2];            // a chain's sums are there; have been taken
   uint32_t tmem_base;
   int abort_flag;
 };
+static_assert(sizeof(F32Bars) <= 256, "barrier block outgrew its reservation");
 
 struct F32Op {
   const float *a, *w, *bias, *residual;
@@ -41,15 +45,25 @@ struct F32Op {
   int lda, ldr, ldc, M, N, K, act;
 };
 
-__device__ __forceinline__ float activate(float x, int act) {
-  if (act == kActGelu) return 0.5f * x * erfcf(-0.70710678118654752f * x);
-  if (act == kActNone) return x;
-  return x / (1.f + expf(-(act == kActSilu ? x : x * fmaf(0.0713548162f, x * x, 1.59576912f))));
+// Eight floats, the first and the second four of which are there or zeros; wide: on a 32-byte boundary, and all or none.
+__device__ __forceinline__ void load_floats(uint32_t (&v)[8], const float* p, bool first, bool second, bool wide) {
+  if (wide) {
+    if (first) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                   : "l"(p));
+      return;
+    }
+  }
+  const uint4 none = make_uint4(0, 0, 0, 0);
+  const uint4 lo = !wide && first ? *reinterpret_cast<const uint4*>(p) : none, hi = !wide && second ? *reinterpret_cast<const uint4*>(p + 4) : none;
+  v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
 }
-
 // Eight floats as three packets of bf16.
-__device__ __forceinline__ void cut(const float4& lo, const float4& hi, uint8_t* at, int plane) {
-  float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+__device__ __forceinline__ void cut(const uint32_t (&x)[8], uint8_t* at, int plane) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x[e]);
 #pragma unroll
   for (int p = 0; p < 3; ++p) {
     uint32_t q[4];
@@ -64,20 +78,24 @@ __device__ __forceinline__ void cut(const float4& lo, const float4& hi, uint8_t*
 }
 
 template <int NT, int S>
-__global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const F32Op o, uint32_t* dev_status) {
-  constexpr int kCols = NT / 4, kItemsW = NT / 64;  // columns of a thread; packets of w of a thread (two of a)
-  constexpr int kPart = kCols / S;                  // columns that a CTA finishes in a thread
+__global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const F32Op o, const bool wide, uint32_t* dev_status) {
+  constexpr int kCols = NT / 4, kPart = kCols / S;  // columns of a thread; of which its CTA finishes
+  constexpr bool kW1 = NT == 128;                   // a packet of w for every thread, else for every second
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  F32Bars* bar = reinterpret_cast<F32Bars*>(smem + 2 * kStageBytes<NT>);
+  F32Bars* bar = reinterpret_cast<F32Bars*>(smem + kSlots * kStageBytes<NT>);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = S > 1 ? (int)cluster_rank() : 0, tile = blockIdx.x / S;
   const int nk = (o.K + kStep - 1) / kStep, first = rank * nk / S, steps = (rank + 1) * nk / S - first;  // (nk >= S: one at least)
+  const int chains = (steps + kChunk - 1) / kChunk;
   const int mb = (o.M + 127) / 128, m0 = tile % mb * 128, n0 = tile / mb * NT;
 
   if (tid == 0) {
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kSlots; ++s) {
       mbar_init(&bar->full[s], kWarps);
+      mbar_init(&bar->empty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
       mbar_init(&bar->done[s], 1);
       mbar_init(&bar->taken[s], kWarps);
     }
@@ -86,7 +104,7 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
   }
   dependency_wait();
   if (tid == 0) release_dependents();
-  if (warp == kWarps) tmem_alloc(&bar->tmem_base, 2 * NT);
+  if (warp == kWarps) tmem_alloc(&bar->tmem_base, 4 * NT);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -100,79 +118,76 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
     if (elect_one()) {
       constexpr uint32_t idesc = idesc_f16(kFmtBF16, kFmtBF16, false, true, 128, NT);
       for (int i = 0; i < steps; ++i) {
-        const int s = i & 1;
-        if (!mbar_wait(&bar->full[s], (i >> 1) & 1, dev_status, abort_flag)) break;
-        if (i >= 2 && !mbar_wait(&bar->taken[s], ((i >> 1) - 1) & 1, dev_status, abort_flag)) break;
+        const int s = i % kSlots, chain = i / kChunk, c = chain & 1;
+        const bool begins = i % kChunk == 0;
+        if (!mbar_wait(&bar->full[s], (i / kSlots) & 1, dev_status, abort_flag)) break;
+        if (begins && chain >= 2 && !mbar_wait(&bar->taken[c], ((chain >> 1) - 1) & 1, dev_status, abort_flag)) break;
         tc_fence_after();
-        const uint32_t aa = smem_u32(smem + s * kStageBytes<NT>), wa = aa + 3 * kPlaneA;
-        constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pw[6] = {0, 2, 1, 0, 1, 0};  // the smallest first
+        const uint32_t aa = smem_u32(smem + s * kStageBytes<NT>), wa = aa + 3 * kPlaneA, large = tmem + c * 2 * NT, small = large + NT;
+        constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pw[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
         for (int p = 0; p < 6; ++p)
 #pragma unroll
           for (int kk = 0; kk < kStep / 16; ++kk)
-            mma_ss(tmem + s * NT, smem_desc_sw128(aa + pa[p] * kPlaneA + kk * 32, 16, 1024),
-                   smem_desc_sw128(wa + pw[p] * (NT / 64 * kSlab) + kk * 2048, kSlab, 1024), idesc, p > 0 || kk > 0);
-        mma_commit(&bar->done[s]);
+            mma_ss(p < 5 ? small : large, smem_desc_sw64(aa + pa[p] * kPlaneA + kk * 32, 16, 512),
+                   smem_desc_sw128(wa + pw[p] * kPlaneW<NT> + kk * 2048, kSlab, 1024), idesc, !begins || kk > 0 || (p > 0 && p < 5));
+        mma_commit(&bar->empty[s]);
+        if (i % kChunk == kChunk - 1 || i == steps - 1) mma_commit(&bar->done[c]);
       }
     }
   } else {
-    float4 xa[2][2], xw[kItemsW][2];
-    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
-    const auto fetch = [&](int step) {
-      const int k0 = (first + step) * kStep;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int i = tid + j * 512, r = m0 + (i >> 3), k = k0 + (i & 7) * 8;
-        const float* at = o.a + (size_t)r * o.lda + k;
-        xa[j][0] = r < o.M && k < o.K ? *reinterpret_cast<const float4*>(at) : none;
-        xa[j][1] = r < o.M && k + 4 < o.K ? *reinterpret_cast<const float4*>(at + 4) : none;
-      }
-#pragma unroll
-      for (int j = 0; j < kItemsW; ++j) {
-        const int i = tid + j * 512, k = k0 + i / (NT / 8), n = n0 + i % (NT / 8) * 8;
-        const float* at = o.w + (size_t)k * o.N + n;
-        xw[j][0] = k < o.K && n < o.N ? *reinterpret_cast<const float4*>(at) : none;
-        xw[j][1] = k < o.K && n + 4 < o.N ? *reinterpret_cast<const float4*>(at + 4) : none;
-      }
+    // a thread's packets of eight: row tid / 4 of a; row of w
+    const int a_row = tid >> 2, a_pk = tid & 3, w_row = tid / (NT / 8), w_pk = tid % (NT / 8);
+    const bool a_in = m0 + a_row < o.M, w_in = (kW1 || tid < 256) && n0 + w_pk * 8 < o.N, w_whole = n0 + w_pk * 8 + 4 < o.N;
+    const float* a_at = o.a + (size_t)(m0 + a_row) * o.lda + a_pk * 8;
+    const float* w_at = o.w + (size_t)w_row * o.N + n0 + w_pk * 8;
+    const uint32_t a_to = (uint32_t)a_row * 64u + (uint32_t)((a_pk ^ ((a_row >> 1) & 3)) << 4);
+    const uint32_t w_to = 3 * kPlaneA + (w_pk >> 3) * kSlab + sw128_offset(w_row, w_pk & 7);
+    uint32_t xa[2][8], xw[2][8];
+    const auto fetch = [&](int step, uint32_t (&a8)[8], uint32_t (&w8)[8]) {
+      const int ka = (first + step) * kStep + a_pk * 8, kw = (first + step) * kStep + w_row;
+      load_floats(a8, a_at + (size_t)(first + step) * kStep, a_in && ka < o.K, a_in && ka + 4 < o.K, wide);
+      load_floats(w8, w_at + (size_t)(first + step) * kStep * o.N, w_in && kw < o.K, w_in && w_whole && kw < o.K, wide);
     };
-    const auto take = [&](int step) {  // the sums of a stage
-      const int s = step & 1;
-      if (!mbar_wait_warp(&bar->done[s], (step >> 1) & 1, dev_status, abort_flag)) return false;
+    const auto take = [&](int chain) {
+      const int c = chain & 1;
+      if (!mbar_wait_warp(&bar->done[c], (chain >> 1) & 1, dev_status, abort_flag)) return false;
       tc_fence_after();
-      uint32_t r[kCols];
-      const uint32_t at = tmem + s * NT + group * kCols + ((uint32_t)(quarter * 32) << 16);
-      if constexpr (kCols == 32) tmem_ld32(at, r);
-      else tmem_ld16(at, r);
-      tmem_wait_ld();
+      const uint32_t at = tmem + c * 2 * NT + group * kCols + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll
+      for (int h = 0; h < kCols; h += 16) {
+        uint32_t large[16], small[16];
+        tmem_ld16(at + h, large);
+        tmem_ld16(at + NT + h, small);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[h + e] += __uint_as_float(large[e]) + __uint_as_float(small[e]);
+      }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bar->taken[s]);
-#pragma unroll
-      for (int e = 0; e < kCols; ++e) acc[e] += __uint_as_float(r[e]);
+      if (lane == 0) mbar_arrive(&bar->taken[c]);
       return true;
     };
-    fetch(0);
-    for (int i = 0; i < steps; ++i) {
-      // (the slot's last products were waited for when their sums were taken)
-      uint8_t* sa = smem + (i & 1) * kStageBytes<NT>;
-      uint8_t* sw = sa + 3 * kPlaneA;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int e = tid + j * 512;
-        cut(xa[j][0], xa[j][1], sa + sw128_offset(e >> 3, e & 7), kPlaneA);
-      }
-#pragma unroll
-      for (int j = 0; j < kItemsW; ++j) {
-        const int e = tid + j * 512, k = e / (NT / 8), p = e % (NT / 8);
-        cut(xw[j][0], xw[j][1], sw + (p >> 3) * kSlab + sw128_offset(k, p & 7), NT / 64 * kSlab);
-      }
+    int taken = 0;
+    const auto turn = [&](int i, uint32_t (&a8)[8], uint32_t (&w8)[8]) {
+      const int s = i % kSlots;
+      if (i >= kSlots && !mbar_wait_warp(&bar->empty[s], (i / kSlots - 1) & 1, dev_status, abort_flag)) return false;
+      uint8_t* at = smem + s * kStageBytes<NT>;
+      cut(a8, at + a_to, kPlaneA);
+      if (kW1 || tid < 256) cut(w8, at + w_to, kPlaneW<NT>);
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bar->full[i & 1]);
-      if (i + 1 < steps) fetch(i + 1);
-      if (i > 0 && !take(i - 1)) { ok = false; break; }
+      if (lane == 0) mbar_arrive(&bar->full[s]);
+      if (i + 2 < steps) fetch(i + 2, a8, w8);
+      return i % kChunk != 2 || i < kChunk || take(taken++);
+    };
+    fetch(0, xa[0], xw[0]);
+    if (steps > 1) fetch(1, xa[1], xw[1]);
+    for (int i = 0; ok && i < steps; i += 2) {
+      ok = turn(i, xa[0], xw[0]);
+      if (ok && i + 1 < steps) ok = turn(i + 1, xa[1], xw[1]);
     }
-    if (ok) ok = take(steps - 1);
+    while (ok && taken < chains) ok = take(taken++);
   }
 
   if constexpr (S > 1) {
@@ -241,7 +256,7 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
       }
       if (o.act != kActNone) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[e + u] = activate(v[e + u], o.act);
+        for (int u = 0; u < 4; ++u) v[e + u] = epi::activate_f32(v[e + u], o.act);
       }
       if (o.residual) {
         const float4 r = *reinterpret_cast<const float4*>(o.residual + (size_t)m * o.ldr + n);
@@ -254,7 +269,7 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
   __syncthreads();
   if (warp == kWarps) {
     tc_fence_after();
-    tmem_dealloc(tmem, 2 * NT);
+    tmem_dealloc(tmem, 4 * NT);
   }
 }
 
@@ -267,26 +282,22 @@ template <int NT, int S>
 cudaError_t run_f32(const F32Op& o, uint32_t* dev_status, cudaStream_t s) {
   const long long ctas = (long long)((o.M + 127) / 128) * ((o.N + NT - 1) / NT) * S;
   if (ctas > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_dependent_cluster(linear_f32_kernel<NT, S>, dim3((unsigned)ctas), dim3((kWarps + 1) * 32), (size_t)kSmem<NT>, S, s, o, dev_status);
+  const bool wide = (((uintptr_t)o.a | (uintptr_t)o.w) & 31) == 0 && o.lda % 8 == 0 && o.N % 8 == 0 && o.K % 8 == 0;
+  return launch_dependent_cluster(linear_f32_kernel<NT, S>, dim3((unsigned)ctas), dim3((kWarps + 1) * 32), (size_t)kSmem<NT>, S, s, o, wide, dev_status);
 }
 
 }  // namespace
 
-// Rows of 16-byte packets: what the kernel loads and stores.
-bool linear_f32_tc_ok(const LinearPlusOp& o) {
-  return o.M > 16 && o.N % 4 == 0 && o.K % 4 == 0 && o.lda % 4 == 0 && o.ldc % 4 == 0 && (!o.residual || o.ldr % 4 == 0);
-}
-
 cudaError_t launch_linear_f32_tc(const LinearPlusOp& l, uint32_t* dev_status, cudaStream_t s) {
   const F32Op o{(const float*)l.a, (const float*)l.w, (const float*)l.bias, (const float*)l.residual, (float*)l.c, l.lda, l.ldr, l.ldc, l.M, l.N, l.K, l.act};
-  const int steps = (l.K + kStep - 1) / kStep;
-  struct Form {
+    struct Form {
     int cols, parts, at_once, launch, step;
     cudaError_t (*run)(const F32Op&, uint32_t*, cudaStream_t);
   };
-  const Form forms[] = {{128, 1, f32_at_once<128, 1>(), 5000, 900, run_f32<128, 1>}, {64, 1, f32_at_once<64, 1>(), 5000, 600, run_f32<64, 1>},
-                        {128, 2, f32_at_once<128, 2>(), 7000, 900, run_f32<128, 2>}, {128, 4, f32_at_once<128, 4>(), 7000, 900, run_f32<128, 4>},
-                        {64, 2, f32_at_once<64, 2>(), 7000, 600, run_f32<64, 2>},    {64, 4, f32_at_once<64, 4>(), 7000, 600, run_f32<64, 4>}};
+  const Form forms[] = {{128, 1, f32_at_once<128, 1>(), 6000, 800, run_f32<128, 1>}, {64, 1, f32_at_once<64, 1>(), 6000, 450, run_f32<64, 1>},
+                        {128, 2, f32_at_once<128, 2>(), 7000, 800, run_f32<128, 2>}, {128, 4, f32_at_once<128, 4>(), 7000, 800, run_f32<128, 4>},
+                        {64, 2, f32_at_once<64, 2>(), 7000, 450, run_f32<64, 2>},    {64, 4, f32_at_once<64, 4>(), 7000, 450, run_f32<64, 4>}};
+  const int steps = (l.K + kStep - 1) / kStep;
   int best = -1;
   long long least = LLONG_MAX;
   const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only

@@ -43,6 +43,46 @@ __device__ __forceinline__ uint4 load16_e4m3(const uint8_t* p, int left) {
 }
 __device__ __forceinline__ uint32_t word(const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
 
+// An eight of columns of a row: the sums of the warps, and of all CTAs of the cluster where `mine`.
+template <int kRows>
+__device__ __forceinline__ void add_up(const float (&part)[kWarps][kRows][kPitch], float (&sums)[8][kRows][8], int split, int rank, int row, int oct,
+                                       bool mine, float (&v)[8]) {
+  const int per = 8 / split;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+  if (row < kRows) {
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(&part[w][row][oct * 8]), y = *reinterpret_cast<const float4*>(&part[w][row][oct * 8 + 4]);
+      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+    }
+  }
+  if (split > 1) {
+    cluster_wait();  // all CTAs have begun
+    if (row < kRows) {
+      // to who finishes this eight, which has per of them a row
+      const uint32_t at = peer_addr(smem_u32(&sums[0][0][0]) + (uint32_t)(((rank * kRows + row) * per + oct % per) * 32), (uint32_t)(oct / per));
+      uint32_t b[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(v[e]);
+      st_peer_v4(at, b);
+      st_peer_v4(at + 16, b + 4);
+    }
+    cluster_arrive();
+    cluster_wait();  // all sums are there, and nobody writes into another's any more
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    if (mine) {
+      for (int r = 0; r < split; ++r) {
+        const float* at = &sums[0][0][0] + ((r * kRows + row) * per + oct % per) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += at[e];
+      }
+    }
+  }
+}
+
 struct RowsOp {
   const void *a, *w;
   int lda, ldw, M, N, K, act, split;
@@ -133,39 +173,75 @@ __global__ void __launch_bounds__(kWarps * 32, 2) linear_rows_kernel(const RowsO
       }
     }
   }
-  __syncthreads();
-  float v[8] = {};
-  if (row < kRows) {
+  float v[8];
+  add_up<kRows>(part, sums, o.split, rank, row, oct, mine, v);
+  if (mine) finish8<kKind>(v, kKind == kPlus8 ? plus.a_scale[row] : 1.f, plus, o.act, res, n, plus.c + (size_t)row * plus.ldc + n);
+}
+
+// The same in fp32 on FFMA: a thread has four columns of w and four consecutive contraction elements of every 64, sixteen threads
+// beside one another the columns, sixteen the elements.
+template <int kRows>
+__global__ void __launch_bounds__(kWarps * 32) linear_rows_f32_kernel(const RowsOp o, const float* bias, const float* residual, float* c, int ldr, int ldc) {
+  __shared__ __align__(16) float part[kWarps][kRows][kPitch];
+  __shared__ __align__(16) float sums[8][kRows][8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = (threadIdx.x & 15) * 4, k_lane = threadIdx.x >> 4;
+  const int rank = o.split > 1 ? (int)cluster_rank() : 0, n0 = (int)(blockIdx.x / o.split) * kBlock;
+  const int steps = (o.K + 63) / 64, first = (int)((long long)steps * rank / o.split), last = (int)((long long)steps * (rank + 1) / o.split);
+  dependency_wait();
+  if (threadIdx.x == 0) release_dependents();
+  if (o.split > 1) cluster_arrive();
+  const int row = threadIdx.x >> 3, oct = threadIdx.x & 7, n = n0 + oct * 8;
+  const bool mine = row < o.M && row < kRows && oct / (8 / o.split) == rank && n < o.N;
+  const bool in_n = n0 + col < o.N;
+  float acc[kRows][4] = {};
+  const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 w[4], a[kRows];
+  const auto load = [&](int step) {
+    const int k = step * 64 + k_lane * 4;
+    const bool in_k = k < o.K;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float4 x = *reinterpret_cast<const float4*>(&part[w][row][oct * 8]), y = *reinterpret_cast<const float4*>(&part[w][row][oct * 8 + 4]);
-      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
-    }
-  }
-  if (o.split > 1) {
-    cluster_wait();  // all CTAs have begun
-    if (row < kRows) {
-      // to who finishes this eight, which has per of them a row
-      const uint32_t at = peer_addr(smem_u32(&sums[0][0][0]) + (uint32_t)(((rank * kRows + row) * per + oct % per) * 32), (uint32_t)(oct / per));
-      uint32_t b[8];
+    for (int e = 0; e < 4; ++e) w[e] = in_k && in_n ? *reinterpret_cast<const float4*>((const float*)o.w + (size_t)(k + e) * o.N + n0 + col) : none;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(v[e]);
-      st_peer_v4(at, b);
-      st_peer_v4(at + 16, b + 4);
-    }
-    cluster_arrive();
-    cluster_wait();  // all sums are there, and nobody writes into another's any more
+    for (int r = 0; r < kRows; ++r) a[r] = in_k && r < o.M ? *reinterpret_cast<const float4*>((const float*)o.a + (size_t)r * o.lda + k) : none;
+  };
+  if (first < last) load(first);
+  for (int s = first; s < last; ++s) {
+    float4 ww[4], aa[kRows];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    if (mine) {
-      for (int r = 0; r < o.split; ++r) {
-        const float* at = &sums[0][0][0] + ((r * kRows + row) * per + oct % per) * 8;
+    for (int e = 0; e < 4; ++e) ww[e] = w[e];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += at[e];
+    for (int r = 0; r < kRows; ++r) aa[r] = a[r];
+    if (s + 1 < last) load(s + 1);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const float x[4] = {aa[r].x, aa[r].y, aa[r].z, aa[r].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[r][0] = fmaf(x[e], ww[e].x, acc[r][0]);
+        acc[r][1] = fmaf(x[e], ww[e].y, acc[r][1]);
+        acc[r][2] = fmaf(x[e], ww[e].z, acc[r][2]);
+        acc[r][3] = fmaf(x[e], ww[e].w, acc[r][3]);
       }
     }
   }
-  if (mine) finish8<kKind>(v, kKind == kPlus8 ? plus.a_scale[row] : 1.f, plus, o.act, res, n, plus.c + (size_t)row * plus.ldc + n);
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[r][e] += __shfl_xor_sync(0xffffffffu, acc[r][e], 16);
+    if (lane < 16) *reinterpret_cast<float4*>(&part[warp][r][col]) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
+  }
+  float v[8];
+  add_up<kRows>(part, sums, o.split, rank, row, oct, mine, v);
+  if (!mine) return;
+#pragma unroll
+  for (int h = 0; h < 8; h += 4) {
+    if (n + h >= o.N) break;
+    const float4 b = bias ? *reinterpret_cast<const float4*>(bias + n + h) : none;
+    const float4 r = residual ? *reinterpret_cast<const float4*>(residual + (size_t)row * ldr + n + h) : none;
+    *reinterpret_cast<float4*>(c + (size_t)row * ldc + n + h) =
+        make_float4(activate_f32(v[h] + b.x, o.act) + r.x, activate_f32(v[h + 1] + b.y, o.act) + r.y, activate_f32(v[h + 2] + b.z, o.act) + r.z,
+                    activate_f32(v[h + 3] + b.w, o.act) + r.w);
+  }
 }
 
 template <int kKind, bool kTall>
@@ -183,6 +259,18 @@ int linear_rows_split(int N, int steps, int sms) {
   int split = 1;
   while (split < 8 && blocks * split * 2 <= 2 * sms && steps >= kWarps * split) split *= 2;
   return split;
+}
+
+cudaError_t launch_linear_rows_f32(const LinearPlusOp& l, cudaStream_t s) {
+  const int blocks = (l.N + kBlock - 1) / kBlock, steps = (l.K + 63) / 64;
+  int split = 1;
+  while (split < 8 && blocks * split * 2 <= 2 * sm_count() && steps >= split * 4) split *= 2;
+  const RowsOp o{l.a, l.w, l.lda, l.ldw, l.M, l.N, l.K, l.act, split};
+  const auto kernel = l.M > 8 ? linear_rows_f32_kernel<16> : linear_rows_f32_kernel<8>;
+  const cudaError_t e = launch_dependent_cluster(kernel, dim3((unsigned)(blocks * split)), dim3(kWarps * 32), 0, split, s, o, (const float*)l.bias,
+                                                 (const float*)l.residual, (float*)l.c, l.ldr, l.ldc);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 cudaError_t launch_linear_rows(const LinearPlusOp& l, int split, cudaStream_t s) {

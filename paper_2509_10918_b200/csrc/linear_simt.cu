@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "linear_epilogue.cuh"
 #include "spread.cuh"
 #include "tc.cuh"
 
@@ -832,8 +833,7 @@ cudaError_t launch_linear_simt(int M, int N, int K, bool f32, const void* a, con
   return cudaGetLastError();
 }
 
-// c = act(a w + bias) + residual in fp32, rows of a, residual and c at strides of their own.  The sigmoid and the tail of the GELU
-// are taken to full precision: fp32 mode is what bf16 runs are checked against.
+// c = act(a w + bias) + residual in fp32, rows of a, residual and c at strides of their own.
 struct LinearPlusF32 {
   static constexpr bool a_k_contig = true;
   typedef const float* APtr;
@@ -852,11 +852,7 @@ struct LinearPlusF32 {
     }
     if (act != kActNone) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = f[e];
-        if (act == kActGelu) f[e] = 0.5f * x * erfcf(-0.70710678118654752f * x);
-        else f[e] = x / (1.f + expf(-(act == kActSilu ? x : x * fmaf(0.0713548162f, x * x, 1.59576912f))));
-      }
+      for (int e = 0; e < 4; ++e) f[e] = epi::activate_f32(f[e], act);
     }
     if (residual) {
       const float4 r = load4(residual + (size_t)m * ldr + n, left, r_vec);

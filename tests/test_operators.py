@@ -441,17 +441,18 @@ def test_linear_q8_parity(toma, m, n, k):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 640, 640), (2, 1280, 320), (5, 7, 1000), (64, 130, 66), (301, 96, 161), (1003, 640, 320)])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 4, 4), (3, 68, 60), (2, 312, 3272), (8, 640, 2560), (9, 132, 5120), (16, 5120, 640), (1, 640, 640), (2, 1280, 320), (5, 7, 1000), (64, 130, 66), (301, 96, 161), (1003, 640, 320)])
 def test_linear_f32_parity(toma, m, n, k):
     run_linear(toma, m, n, k, F32, True, "gelu", True)
     run_linear(toma, m, n, k, F32, False, "silu", False, pad=5, seed=1)
+    run_linear(toma, m, n, k, F32, True, "none", True, pad=4, seed=2)
 
 
 F32_SHAPES = [(17, 4, 4), (20, 640, 2560), (128, 64, 64), (130, 200, 132), (300, 72, 1000), (515, 1284, 68), (1003, 2560, 640), (2048, 320, 2560), (64, 64, 20000)]
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("form", [0, 1, 2, 3, 4, 5, 6], ids=["chosen", "128", "64", "128split2", "128split4", "64split2", "64split4"])
+@pytest.mark.parametrize("form", range(7), ids=["chosen", "128", "64", "128split2", "128split4", "64split2", "64split4"])
 def test_linear_f32_on_the_tensor_cores(toma, tuning, form):
     """Floats as sums of three bf16 numbers: the bound of a sum in fp32, the length of the longest among them."""
     tuning(linear_tile=form)
