@@ -520,7 +520,7 @@ static cudaError_t do_linear_plus(const LinearPlusOp& o, bool f32, uint32_t* dev
   if (!f32) return launch_linear_plus_tc(o, dev_status, s);
   // (without rows of 16-byte packets, which the other kernels load and store)
   if (o.N % 4 || o.K % 4 || o.lda % 4 || o.ldc % 4 || (o.residual && o.ldr % 4)) return launch_linear_plus_simt(o, s);
-  return o.M > 16 ? launch_linear_f32_tc(o, dev_status, s) : launch_linear_rows_f32(o, s);
+  return o.M > 16 ? launch_linear_f32_tc(o, dev_status, s) : launch_linear_rows(o, true, s);
 }
 
 toma_status toma_linear_act(int32_t m, int32_t n, int32_t k, int32_t dtype, const void* a, int32_t lda, const void* w, const void* bias, int32_t act,

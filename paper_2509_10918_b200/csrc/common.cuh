@@ -155,12 +155,10 @@ struct PlusDevice {
 // split, 128 x 128 by 2, 4, 8 CTAs (6, 7, 8) or 256 x 256 by 2, 3 pairs (9, 10).  `steps`: of 128 bytes of a row.
 int linear_plus_form(int M, int N, int steps, int act, const PlusDevice& d);
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
-// At most 16 rows, `split` CTAs (1, 2, 4 or 8) for the contraction of 64 columns.
-int linear_rows_split(int N, int steps, int sms);
-cudaError_t launch_linear_rows(const LinearPlusOp& o, int split, cudaStream_t s);
-// fp32: any shape on FFMA; rows of 16-byte packets: at most 16, or on the tensor cores.
+// At most 16 rows (fp32: of 16-byte packets).
+cudaError_t launch_linear_rows(const LinearPlusOp& o, bool f32, cudaStream_t s);
+// fp32: any shape on FFMA; rows of 16-byte packets on the tensor cores.
 cudaError_t launch_linear_plus_simt(const LinearPlusOp& o, cudaStream_t s);
-cudaError_t launch_linear_rows_f32(const LinearPlusOp& o, cudaStream_t s);
 cudaError_t launch_linear_f32_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
 // w [K][N] bf16 -> q [N][K] e4m3 (row stride ldq) with scale [N].
 cudaError_t launch_quantise_weight(int K, int N, const void* w, void* q, int ldq, float* scale, cudaStream_t s);

@@ -1052,7 +1052,7 @@ int linear_plus_form(int M, int N, int steps, int act, const PlusDevice& d) {
 // c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
   const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
-  if (o.M <= 16 && (tune == 0 || tune == 1)) return launch_linear_rows(o, linear_rows_split(o.N, (o.K + (o.f8 ? 63 : 31)) / (o.f8 ? 64 : 32), sm_count()), s);
+  if (o.M <= 16 && (tune == 0 || tune == 1)) return launch_linear_rows(o, false, s);
   CUtensorMap ta, tw;
   const uint64_t adims[2] = {(uint64_t)o.K, (uint64_t)o.M}, astr[1] = {(uint64_t)o.lda * (o.f8 ? 1 : 2)};
   const uint32_t abox[2] = {o.f8 ? 128u : 64u, 128};

@@ -7,9 +7,11 @@
 // of their own, and the chains' sums are added up by the threads, rounded: 512 x 256 x 640 is 1.6 units of 2^-24 off 64 bits
 // (root mean square), 7.6 on FFMA.  Six bf16 products run at some 375 TFLOP/s, FFMA at 75.
 //
-// A CTA has a tile of 128 x 128 or 128 x 64.  Sixteen warps take the floats from global memory, two stages of 32 contraction elements ahead
-// in registers, cut them into three planes each in shared memory (four stages) and add up the chains' sums, 32 or 16 columns
-// of a row a thread; a seventeenth issues the MMAs.  Where there are few tiles a cluster of 2 or 4 CTAs splits the contraction
+// A CTA has a tile of 128 x 128 or 128 x 64.  Two groups of eight warps take the floats of every second stage of 32 contraction elements from
+// global memory, the group's next stage in registers meanwhile, and cut them into three planes each in shared memory (four
+// stages); a stage is a chain of latencies for a warp, which the other group's stage covers (sixteen warps on every stage took
+// 1900 cycles for each, whose instructions take 650 and MMAs 770).  All sixteen add up the chains' sums, 32 or 16 columns of a row a
+// thread; a seventeenth issues the MMAs.  Where there are few tiles a cluster of 2 or 4 CTAs splits the contraction
 // and exchanges its parts through distributed shared memory.
 #include <climits>
 
@@ -80,7 +82,7 @@ __device__ __forceinline__ void cut(const uint32_t (&x)[8], uint8_t* at, int pla
 template <int NT, int S>
 __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const F32Op o, const bool wide, uint32_t* dev_status) {
   constexpr int kCols = NT / 4, kPart = kCols / S;  // columns of a thread; of which its CTA finishes
-  constexpr bool kW1 = NT == 128;                   // a packet of w for every thread, else for every second
+  constexpr int kPacksW = NT / 64;                  // packets of eight of w of a thread and stage (two of a)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   F32Bars* bar = reinterpret_cast<F32Bars*>(smem + kSlots * kStageBytes<NT>);
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
 
   if (tid == 0) {
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(&bar->full[s], kWarps);
+      mbar_init(&bar->full[s], kWarps / 2);
       mbar_init(&bar->empty[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
@@ -136,18 +138,26 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
       }
     }
   } else {
-    // a thread's packets of eight: row tid / 4 of a; row of w
-    const int a_row = tid >> 2, a_pk = tid & 3, w_row = tid / (NT / 8), w_pk = tid % (NT / 8);
-    const bool a_in = m0 + a_row < o.M, w_in = (kW1 || tid < 256) && n0 + w_pk * 8 < o.N, w_whole = n0 + w_pk * 8 + 4 < o.N;
+    // a thread's packets of eight: rows t / 4 and 64 further on of a; of w a row of 128 columns and 16 further on, or of 64
+    const int half = warp >> 3, t = tid & 255, a_row = t >> 2, a_pk = t & 3, w_row = t / (NT / 8), w_pk = t % (NT / 8);
+    const bool w_in = n0 + w_pk * 8 < o.N, w_whole = n0 + w_pk * 8 + 4 < o.N;
     const float* a_at = o.a + (size_t)(m0 + a_row) * o.lda + a_pk * 8;
     const float* w_at = o.w + (size_t)w_row * o.N + n0 + w_pk * 8;
     const uint32_t a_to = (uint32_t)a_row * 64u + (uint32_t)((a_pk ^ ((a_row >> 1) & 3)) << 4);
     const uint32_t w_to = 3 * kPlaneA + (w_pk >> 3) * kSlab + sw128_offset(w_row, w_pk & 7);
-    uint32_t xa[2][8], xw[2][8];
-    const auto fetch = [&](int step, uint32_t (&a8)[8], uint32_t (&w8)[8]) {
-      const int ka = (first + step) * kStep + a_pk * 8, kw = (first + step) * kStep + w_row;
-      load_floats(a8, a_at + (size_t)(first + step) * kStep, a_in && ka < o.K, a_in && ka + 4 < o.K, wide);
-      load_floats(w8, w_at + (size_t)(first + step) * kStep * o.N, w_in && kw < o.K, w_in && w_whole && kw < o.K, wide);
+    uint32_t xa[2][8], xw[kPacksW][8];
+    const auto fetch = [&](int step) {
+      const int k0 = (first + step) * kStep, ka = k0 + a_pk * 8;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const bool in = m0 + a_row + 64 * j < o.M;
+        load_floats(xa[j], a_at + (size_t)64 * j * o.lda + k0, in && ka < o.K, in && ka + 4 < o.K, wide);
+      }
+#pragma unroll
+      for (int j = 0; j < kPacksW; ++j) {
+        const bool in = k0 + w_row + 16 * j < o.K;
+        load_floats(xw[j], w_at + (size_t)(k0 + 16 * j) * o.N, w_in && in, w_whole && in, wide);
+      }
     };
     const auto take = [&](int chain) {
       const int c = chain & 1;
@@ -169,23 +179,20 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
       return true;
     };
     int taken = 0;
-    const auto turn = [&](int i, uint32_t (&a8)[8], uint32_t (&w8)[8]) {
+    if (half < steps) fetch(half);
+    for (int i = half; ok && i < steps; i += 2) {
       const int s = i % kSlots;
-      if (i >= kSlots && !mbar_wait_warp(&bar->empty[s], (i / kSlots - 1) & 1, dev_status, abort_flag)) return false;
+      if (i >= kSlots && !mbar_wait_warp(&bar->empty[s], (i / kSlots - 1) & 1, dev_status, abort_flag)) { ok = false; break; }
       uint8_t* at = smem + s * kStageBytes<NT>;
-      cut(a8, at + a_to, kPlaneA);
-      if (kW1 || tid < 256) cut(w8, at + w_to, kPlaneW<NT>);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) cut(xa[j], at + a_to + j * 64 * 64, kPlaneA);
+#pragma unroll
+      for (int j = 0; j < kPacksW; ++j) cut(xw[j], at + w_to + j * 16 * 128, kPlaneW<NT>);
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar->full[s]);
-      if (i + 2 < steps) fetch(i + 2, a8, w8);
-      return i % kChunk != 2 || i < kChunk || take(taken++);
-    };
-    fetch(0, xa[0], xw[0]);
-    if (steps > 1) fetch(1, xa[1], xw[1]);
-    for (int i = 0; ok && i < steps; i += 2) {
-      ok = turn(i, xa[0], xw[0]);
-      if (ok && i + 1 < steps) ok = turn(i + 1, xa[1], xw[1]);
+      if (i + 2 < steps) fetch(i + 2);
+      if (i % kChunk >= 2 && i >= kChunk) ok = take(taken++);  // the chain before
     }
     while (ok && taken < chains) ok = take(taken++);
   }
@@ -294,9 +301,11 @@ cudaError_t launch_linear_f32_tc(const LinearPlusOp& l, uint32_t* dev_status, cu
     int cols, parts, at_once, launch, step;
     cudaError_t (*run)(const F32Op&, uint32_t*, cudaStream_t);
   };
-  const Form forms[] = {{128, 1, f32_at_once<128, 1>(), 6000, 800, run_f32<128, 1>}, {64, 1, f32_at_once<64, 1>(), 6000, 450, run_f32<64, 1>},
-                        {128, 2, f32_at_once<128, 2>(), 7000, 800, run_f32<128, 2>}, {128, 4, f32_at_once<128, 4>(), 7000, 800, run_f32<128, 4>},
-                        {64, 2, f32_at_once<64, 2>(), 7000, 450, run_f32<64, 2>},    {64, 4, f32_at_once<64, 4>(), 7000, 450, run_f32<64, 4>}};
+  // Rounds of tiles, each a fixed part and a part per stage: nanoseconds, fitted to 20 shapes between 20 x 312 x 3272 and 4096 x 2560 x 640
+  // that were timed in every form (the form named takes at most 1.07 times as long as the best).
+  const Form forms[] = {{128, 1, f32_at_once<128, 1>(), 9600, 810, run_f32<128, 1>}, {64, 1, f32_at_once<64, 1>(), 6000, 530, run_f32<64, 1>},
+                        {128, 2, f32_at_once<128, 2>(), 8600, 740, run_f32<128, 2>}, {128, 4, f32_at_once<128, 4>(), 8000, 790, run_f32<128, 4>},
+                        {64, 2, f32_at_once<64, 2>(), 6100, 540, run_f32<64, 2>},    {64, 4, f32_at_once<64, 4>(), 5800, 570, run_f32<64, 4>}};
   const int steps = (l.K + kStep - 1) / kStep;
   int best = -1;
   long long least = LLONG_MAX;

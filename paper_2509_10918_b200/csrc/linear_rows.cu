@@ -11,6 +11,7 @@
 //   e4m3, w [n][k]: 64 elements at a time, thread t has elements 16 t .. 16 t + 15, 16 bytes of a column, and of a row of a.
 // The warps' sums are added up through shared memory, the CTAs' through distributed shared memory, in a fixed order.
 // 2 x 5120 x 1280 in bf16 (13 MB of weights, out of L2): TODO us.
+#include "clusters.cuh"
 #include "linear_epilogue.cuh"
 
 namespace toma {
@@ -244,40 +245,48 @@ __global__ void __launch_bounds__(kWarps * 32) linear_rows_f32_kernel(const Rows
   }
 }
 
+// CTAs that split a block's contraction (1, 2, 4 or 8): twice the SMs in all at most, `least` steps for each, and as many as the device
+// places beside one another.
+template <typename Kernel>
+int split_of(Kernel kernel, ClusterState (&st)[3], int N, int steps, int least) {
+  const int blocks = (N + kBlock - 1) / kBlock;
+  int split = 1;
+  for (int i = 0; i < 3 && blocks * split * 2 <= 2 * sm_count() && steps >= least * split; ++i) {
+    if (clusters_at_once(kernel, st[i], 2 << i, kWarps * 32, 0) < 1) break;
+    split *= 2;
+  }
+  return split;
+}
+
+template <int kRows>
+cudaError_t run_rows_f32(const LinearPlusOp& l, cudaStream_t s) {
+  static ClusterState st[3];
+  const int blocks = (l.N + kBlock - 1) / kBlock, split = split_of(linear_rows_f32_kernel<kRows>, st, l.N, (l.K + 63) / 64, 4);
+  const RowsOp o{l.a, l.w, l.lda, l.ldw, l.M, l.N, l.K, l.act, split};
+  return launch_dependent_cluster(linear_rows_f32_kernel<kRows>, dim3((unsigned)(blocks * split)), dim3(kWarps * 32), 0, split, s, o, (const float*)l.bias,
+                                  (const float*)l.residual, (float*)l.c, l.ldr, l.ldc);
+}
+
 template <int kKind, bool kTall>
-cudaError_t run_rows(const RowsOp& o, const LinearPlus& plus, cudaStream_t s) {
-  const dim3 grid((unsigned)((o.N + kBlock - 1) / kBlock) * o.split), block(kWarps * 32);
-  return o.split > 1 ? launch_dependent_cluster(linear_rows_kernel<kKind, kTall>, grid, block, 0, o.split, s, o, plus)
-                     : launch_dependent(linear_rows_kernel<kKind, kTall>, grid, block, 0, s, o, plus);
+cudaError_t run_rows(const LinearPlusOp& l, const LinearPlus& plus, cudaStream_t s) {
+  static ClusterState st[3];
+  const int step = kKind == kPlus8 ? 64 : 32, split = split_of(linear_rows_kernel<kKind, kTall>, st, l.N, (l.K + step - 1) / step, kWarps);
+  const RowsOp o{l.a, l.w, l.lda, l.ldw, l.M, l.N, l.K, l.act, split};
+  return launch_dependent_cluster(linear_rows_kernel<kKind, kTall>, dim3((unsigned)((l.N + kBlock - 1) / kBlock) * split), dim3(kWarps * 32), 0, split, s, o,
+                                  plus);
 }
 
 }  // namespace
 
-// CTAs that split a block's contraction: twice the SMs in all at most, with a step for every warp.
-int linear_rows_split(int N, int steps, int sms) {
-  const int blocks = (N + kBlock - 1) / kBlock;
-  int split = 1;
-  while (split < 8 && blocks * split * 2 <= 2 * sms && steps >= kWarps * split) split *= 2;
-  return split;
-}
-
-cudaError_t launch_linear_rows_f32(const LinearPlusOp& l, cudaStream_t s) {
-  const int blocks = (l.N + kBlock - 1) / kBlock, steps = (l.K + 63) / 64;
-  int split = 1;
-  while (split < 8 && blocks * split * 2 <= 2 * sm_count() && steps >= split * 4) split *= 2;
-  const RowsOp o{l.a, l.w, l.lda, l.ldw, l.M, l.N, l.K, l.act, split};
-  const auto kernel = l.M > 8 ? linear_rows_f32_kernel<16> : linear_rows_f32_kernel<8>;
-  const cudaError_t e = launch_dependent_cluster(kernel, dim3((unsigned)(blocks * split)), dim3(kWarps * 32), 0, split, s, o, (const float*)l.bias,
-                                                 (const float*)l.residual, (float*)l.c, l.ldr, l.ldc);
-  count_launch();
-  return e != cudaSuccess ? e : cudaGetLastError();
-}
-
-cudaError_t launch_linear_rows(const LinearPlusOp& l, int split, cudaStream_t s) {
-  const LinearPlus plus{(const __nv_bfloat16*)l.bias, (const __nv_bfloat16*)l.residual, l.a_scale, l.w_scale, (__nv_bfloat16*)l.c, l.ldc, l.ldr};
-  const RowsOp o{l.a, l.w, l.lda, l.ldw, l.M, l.N, l.K, l.act, split};
-  const cudaError_t e = l.f8 ? (l.M > 8 ? run_rows<kPlus8, true>(o, plus, s) : run_rows<kPlus8, false>(o, plus, s))
-                             : (l.M > 8 ? run_rows<kPlus, true>(o, plus, s) : run_rows<kPlus, false>(o, plus, s));
+cudaError_t launch_linear_rows(const LinearPlusOp& l, bool f32, cudaStream_t s) {
+  cudaError_t e;
+  if (f32) {
+    e = l.M > 8 ? run_rows_f32<16>(l, s) : run_rows_f32<8>(l, s);
+  } else {
+    const LinearPlus plus{(const __nv_bfloat16*)l.bias, (const __nv_bfloat16*)l.residual, l.a_scale, l.w_scale, (__nv_bfloat16*)l.c, l.ldc, l.ldr};
+    e = l.f8 ? (l.M > 8 ? run_rows<kPlus8, true>(l, plus, s) : run_rows<kPlus8, false>(l, plus, s))
+             : (l.M > 8 ? run_rows<kPlus, true>(l, plus, s) : run_rows<kPlus, false>(l, plus, s));
+  }
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -862,9 +862,12 @@ struct LinearPlusF32 {
   }
 };
 cudaError_t launch_linear_plus_simt(const LinearPlusOp& o, cudaStream_t s) {
-  const LinearPlusF32 op{o.M, o.N, o.K, o.lda % 4 == 0, o.N % 4 == 0, o.ldc % 4 == 0, o.ldr % 4 == 0, (const float*)o.a, (const float*)o.w,
-                         (const float*)o.bias, (const float*)o.residual, (float*)o.c, o.lda, o.ldr, o.ldc, o.act};
-  run_gemm(op, 1, s);
+  for (int m = 0; m < o.M; m += 1 << 20) {  // (a grid has 65535 blocks of rows at most)
+    const LinearPlusF32 op{o.M - m < 1 << 20 ? o.M - m : 1 << 20, o.N, o.K, o.lda % 4 == 0, o.N % 4 == 0, o.ldc % 4 == 0, o.ldr % 4 == 0,
+                           (const float*)o.a + (size_t)m * o.lda, (const float*)o.w, (const float*)o.bias,
+                           o.residual ? (const float*)o.residual + (size_t)m * o.ldr : nullptr, (float*)o.c + (size_t)m * o.ldc, o.lda, o.ldr, o.ldc, o.act};
+    run_gemm(op, 1, s);
+  }
   return cudaGetLastError();
 }
 
