@@ -44,7 +44,7 @@ static_assert(sizeof(F32Bars) <= 256, "barrier block outgrew its reservation");
 struct F32Op {
   const float *a, *w, *bias, *residual;
   float* c;
-  int lda, ldr, ldc, M, N, K, act;
+  int lda, ldw, ldr, ldc, M, N, K, act;
 };
 
 // Eight floats, the first and the second four of which are there or zeros; wide: on a 32-byte boundary, and all or none.
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
     const int half = warp >> 3, t = tid & 255, a_row = t >> 2, a_pk = t & 3, w_row = t / (NT / 8), w_pk = t % (NT / 8);
     const bool w_in = n0 + w_pk * 8 < o.N, w_whole = n0 + w_pk * 8 + 4 < o.N;
     const float* a_at = o.a + (size_t)(m0 + a_row) * o.lda + a_pk * 8;
-    const float* w_at = o.w + (size_t)w_row * o.N + n0 + w_pk * 8;
+    const float* w_at = o.w + (size_t)w_row * o.ldw + n0 + w_pk * 8;
     const uint32_t a_to = (uint32_t)a_row * 64u + (uint32_t)((a_pk ^ ((a_row >> 1) & 3)) << 4);
     const uint32_t w_to = 3 * kPlaneA + (w_pk >> 3) * kSlab + sw128_offset(w_row, w_pk & 7);
     uint32_t xa[2][8], xw[kPacksW][8];
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
 #pragma unroll
       for (int j = 0; j < kPacksW; ++j) {
         const bool in = k0 + w_row + 16 * j < o.K;
-        load_floats(xw[j], w_at + (size_t)(k0 + 16 * j) * o.N, w_in && in, w_whole && in, wide);
+        load_floats(xw[j], w_at + (size_t)(k0 + 16 * j) * o.ldw, w_in && in, w_whole && in, wide);
       }
     };
     const auto take = [&](int chain) {
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
       for (int e = 0; e < kPart; ++e)
         if (n_first + e < o.N && !(fabsf(v[e]) < INFINITY)) {
           v[e] = none ? __uint_as_float(0x7FC00000u) : 0.f;
-          for (int k = none ? o.K : 0; k < o.K; ++k) v[e] = fmaf(row[k], o.w[(size_t)k * o.N + n_first + e], v[e]);
+          for (int k = none ? o.K : 0; k < o.K && v[e] == v[e]; ++k) v[e] = fmaf(row[k], o.w[(size_t)k * o.ldw + n_first + e], v[e]);
         }
     }
 #pragma unroll
@@ -283,43 +283,84 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
 template <int NT, int S>
 int f32_at_once() {
   static ClusterState st;
+  if (S == 1) return sm_count();  // (a CTA's shared memory is an SM's)
   return clusters_at_once(linear_f32_kernel<NT, S>, st, S, (kWarps + 1) * 32, kSmem<NT>);
 }
 template <int NT, int S>
 cudaError_t run_f32(const F32Op& o, uint32_t* dev_status, cudaStream_t s) {
   const long long ctas = (long long)((o.M + 127) / 128) * ((o.N + NT - 1) / NT) * S;
   if (ctas > INT32_MAX) return cudaErrorInvalidValue;
-  const bool wide = (((uintptr_t)o.a | (uintptr_t)o.w) & 31) == 0 && o.lda % 8 == 0 && o.N % 8 == 0 && o.K % 8 == 0;
+  static std::atomic<unsigned long long> raised{0};
+  if (cudaError_t e = raise_dynamic_smem(linear_f32_kernel<NT, S>, kSmem<NT>, raised); e != cudaSuccess) return e;
+  const bool wide = (((uintptr_t)o.a | (uintptr_t)o.w) & 31) == 0 && o.lda % 8 == 0 && o.ldw % 8 == 0 && o.N % 8 == 0 && o.K % 8 == 0;
+  if (S == 1) return launch_dependent(linear_f32_kernel<NT, S>, dim3((unsigned)ctas), dim3((kWarps + 1) * 32), (size_t)kSmem<NT>, s, o, wide, dev_status);
   return launch_dependent_cluster(linear_f32_kernel<NT, S>, dim3((unsigned)ctas), dim3((kWarps + 1) * 32), (size_t)kSmem<NT>, S, s, o, wide, dev_status);
+}
+
+// Rounds of tiles, each a fixed part and a part per stage: nanoseconds, fitted to 20 shapes between 20 x 312 x 3272 and 4096 x 2560 x 640
+// that were timed in every form (the form named takes at most 1.07 times as long as the best).
+struct F32Form {
+  int cols, parts, at_once, round, step;
+  cudaError_t (*run)(const F32Op&, uint32_t*, cudaStream_t);
+};
+struct F32Choice {
+  int form;
+  long long cost;
+};
+F32Choice f32_choice(const F32Form (&forms)[6], int M, int N, int steps) {
+  F32Choice best{-1, LLONG_MAX};
+  for (int i = 0; i < 6; ++i) {
+    const F32Form& f = forms[i];
+    if (f.at_once < 1 || steps < f.parts) continue;
+    const long long tiles = (long long)((M + 127) / 128) * ((N + f.cols - 1) / f.cols);
+    const long long cost = (tiles + f.at_once - 1) / f.at_once * (f.round + (long long)((steps + f.parts - 1) / f.parts) * f.step);
+    if (cost < best.cost) best = F32Choice{i, cost};
+  }
+  return best;
 }
 
 }  // namespace
 
+// Where the last round of tiles of 128 x 128 would leave most SMs idle, the columns (or rows) of the whole rounds are one launch and
+// the rest is another, in the form that suits it: 1003 x 2560 x 640, 160 tiles on 148 SMs, 38 us instead of 52.
 cudaError_t launch_linear_f32_tc(const LinearPlusOp& l, uint32_t* dev_status, cudaStream_t s) {
-  const F32Op o{(const float*)l.a, (const float*)l.w, (const float*)l.bias, (const float*)l.residual, (float*)l.c, l.lda, l.ldr, l.ldc, l.M, l.N, l.K, l.act};
-    struct Form {
-    int cols, parts, at_once, launch, step;
-    cudaError_t (*run)(const F32Op&, uint32_t*, cudaStream_t);
-  };
-  // Rounds of tiles, each a fixed part and a part per stage: nanoseconds, fitted to 20 shapes between 20 x 312 x 3272 and 4096 x 2560 x 640
-  // that were timed in every form (the form named takes at most 1.07 times as long as the best).
-  const Form forms[] = {{128, 1, f32_at_once<128, 1>(), 9600, 810, run_f32<128, 1>}, {64, 1, f32_at_once<64, 1>(), 6000, 530, run_f32<64, 1>},
-                        {128, 2, f32_at_once<128, 2>(), 8600, 740, run_f32<128, 2>}, {128, 4, f32_at_once<128, 4>(), 8000, 790, run_f32<128, 4>},
-                        {64, 2, f32_at_once<64, 2>(), 6100, 540, run_f32<64, 2>},    {64, 4, f32_at_once<64, 4>(), 5800, 570, run_f32<64, 4>}};
-  const int steps = (l.K + kStep - 1) / kStep;
-  int best = -1;
-  long long least = LLONG_MAX;
-  const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
-  for (int i = 0; i < 6; ++i) {
-    const Form& f = forms[i];
-    if (f.at_once < 1 || steps < f.parts) continue;
-    const long long tiles = (long long)((l.M + 127) / 128) * ((l.N + f.cols - 1) / f.cols);
-    const long long cost = (tiles + f.at_once - 1) / f.at_once * (f.launch + (long long)((steps + f.parts - 1) / f.parts) * f.step);
-    if (cost < least || tune == i + 1) least = tune == i + 1 ? -1 : cost, best = i;
+  const F32Op whole{(const float*)l.a, (const float*)l.w, (const float*)l.bias, (const float*)l.residual, (float*)l.c, l.lda, l.ldw, l.ldr, l.ldc, l.M, l.N, l.K, l.act};
+  const F32Form forms[] = {{128, 1, f32_at_once<128, 1>(), 9600, 810, run_f32<128, 1>}, {64, 1, f32_at_once<64, 1>(), 6000, 530, run_f32<64, 1>},
+                           {128, 2, f32_at_once<128, 2>(), 8600, 740, run_f32<128, 2>}, {128, 4, f32_at_once<128, 4>(), 8000, 790, run_f32<128, 4>},
+                           {64, 2, f32_at_once<64, 2>(), 6100, 540, run_f32<64, 2>},    {64, 4, f32_at_once<64, 4>(), 5800, 570, run_f32<64, 4>}};
+  const int steps = (l.K + kStep - 1) / kStep, mb = (l.M + 127) / 128, nb = (l.N + 127) / 128;
+  F32Choice one = f32_choice(forms, l.M, l.N, steps), rest{-1, 0};
+  F32Op first = whole, second = whole;
+  if (const int tune = g_tune_linear_tile.load(std::memory_order_relaxed); tune >= 1 && tune <= 6) {  // test-only
+    if (forms[tune - 1].at_once > 0 && steps >= forms[tune - 1].parts) one.form = tune - 1;
+  } else if (const int at_once = forms[0].at_once; at_once > 0) {
+    const long long rounds = (long long)mb * nb / at_once;
+    const bool by_columns = mb <= at_once;
+    const int blocks = (int)(rounds * at_once / (by_columns ? mb : nb)) * 128;  // columns (rows) of the whole rounds
+    if (blocks > 0 && blocks < (by_columns ? l.N : l.M)) {
+      F32Op f = whole, r = whole;
+      if (by_columns) {
+        f.N = blocks, r.N -= blocks;
+        r.w += blocks, r.c += blocks;
+        if (r.bias) r.bias += blocks;
+        if (r.residual) r.residual += blocks;
+      } else {
+        f.M = blocks, r.M -= blocks;
+        r.a += (size_t)blocks * r.lda, r.c += (size_t)blocks * r.ldc;
+        if (r.residual) r.residual += (size_t)blocks * r.ldr;
+      }
+      const F32Choice behind = f32_choice(forms, r.M, r.N, steps);
+      const long long cost = rounds * (forms[0].round + (long long)steps * forms[0].step) + behind.cost;
+      if (behind.form >= 0 && cost < one.cost) one = F32Choice{0, cost}, rest = behind, first = f, second = r;
+    }
   }
-  if (best < 0) return cudaErrorInvalidValue;
-  const cudaError_t e = forms[best].run(o, dev_status, s);
+  if (one.form < 0) return cudaErrorInvalidValue;
+  cudaError_t e = forms[one.form].run(first, dev_status, s);
   count_launch();
+  if (e == cudaSuccess && rest.form >= 0) {
+    e = forms[rest.form].run(second, dev_status, s);
+    count_launch();
+  }
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

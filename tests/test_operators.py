@@ -47,7 +47,8 @@ def to_e4m3(v):
     where top has a factor 7: 145 / 280 comes out above 232 / 448.)"""
     values = e4m3_values(v.device)
     middles = (values[1:] + values[:-1]) / 2
-    low, high = torch.searchsorted(middles, v.abs()), torch.searchsorted(middles, v.abs(), right=True)
+    size = v.abs().contiguous()
+    low, high = torch.searchsorted(middles, size), torch.searchsorted(middles, size, right=True)
     return torch.sign(v) * values[torch.where(low % 2 == 0, low, high)]
 
 
@@ -448,7 +449,7 @@ def test_linear_f32_parity(toma, m, n, k):
     run_linear(toma, m, n, k, F32, True, "none", True, pad=4, seed=2)
 
 
-F32_SHAPES = [(17, 4, 4), (20, 640, 2560), (128, 64, 64), (130, 200, 132), (300, 72, 1000), (515, 1284, 68), (1003, 2560, 640), (2048, 320, 2560), (64, 64, 20000)]
+F32_SHAPES = [(17, 4, 4), (20, 640, 2560), (128, 64, 64), (130, 200, 132), (300, 72, 1000), (515, 1284, 68), (1003, 2560, 640), (2048, 320, 2560), (64, 64, 20000), (20000, 132, 40)]
 
 
 @pytest.mark.gpu
@@ -570,6 +571,70 @@ def test_quantise_weight(toma, k, n):
     want = to_e4m3(p * 448 / top.clamp_min(1e-300)[:, None])
     assert torch.equal(q.double(), want) and ok()
     assert bool(((scale.double() - top / 448).abs() <= top / 448 * 2.0 ** -22).all())
+
+
+@pytest.mark.gpu
+def test_rows_beyond_32_bits_of_elements(toma):
+    """Strided rows whose offsets pass 2^31 elements: the last rows are the ones that a 32-bit offset would miss."""
+    rows, ld, dim = 40000, 65536, 64
+    g = generator(12)
+    buf = torch.zeros(rows, ld, dtype=BF16, device="cuda")
+    x, y = buf[:, :dim], buf[:, 1024:1024 + dim]
+    x.copy_(rand(g, rows, dim))
+    toma.toma_rms_norm(x, None, y)
+    a, c = x, buf[:, 2048:2048 + 72]
+    w = rand(g, dim, 72, dtype=BF16)
+    toma.toma_linear_act(a, w, c, act="silu", residual=buf[:, 4096:4096 + 72])
+    torch.cuda.synchronize()
+    for part in (slice(0, 300), slice(32700, 33000), slice(rows - 300, rows)):
+        want = norm(x[part], None, 1e-6)
+        assert bool(((y[part].double() - want).abs() <= want.abs() * 2.0 ** -7).all())
+        assert_linear(c[part], a[part], w, None, "silu")
+    del buf, x, y, a, c
+    f = torch.zeros(rows, ld, device="cuda")
+    for n in (72, 73):  # on the tensor cores and not
+        w = rand(g, dim, n)
+        f[:, :dim].copy_(rand(g, rows, dim))
+        toma.toma_linear_act(f[:, :dim], w, f[:, 2048:2048 + n])
+        torch.cuda.synchronize()
+        for part in (slice(0, 300), slice(rows - 300, rows)):
+            assert_linear(f[part, 2048:2048 + n], f[part, :dim], w)
+
+
+@pytest.mark.gpu
+def test_binding_refuses_what_it_can_see(toma):
+    x, w, c, b = (torch.zeros(*s, dtype=BF16, device="cuda") for s in ((4, 64), (64, 32), (4, 32), (32,)))
+    toma.toma_linear_act(x, w, c, bias=b)
+    for bad in (dict(a=x.cpu()), dict(a=x[0]), dict(w=w.t()), dict(w=w[:32]), dict(c=c.float()), dict(c=c[:3]), dict(bias=b[:8]), dict(bias=b[::2].repeat(2)[::2]),
+                dict(residual=c.t()), dict(a=x.half()), dict(residual=x), dict(bias=b.float()), dict(a=x.repeat(1, 2)[:, ::2])):
+        args = dict(a=x, w=w, c=c, bias=b)
+        args.update(bad)
+        with pytest.raises(ValueError):
+            toma.toma_linear_act(**args)
+    with pytest.raises(toma.TomaError):
+        toma.toma_linear_act(x, w, c, act="relu")
+    with pytest.raises(toma.TomaError):
+        toma.toma_rms_norm(x, None, x, eps=0.0)
+    with pytest.raises(ValueError):
+        toma.toma_rms_norm(x, None, c)
+    with pytest.raises(ValueError):
+        toma.toma_rms_norm_q8(x, None, torch.zeros(4, 64, dtype=torch.uint8, device="cuda"), torch.zeros(4, device="cuda"))
+    with pytest.raises(ValueError):
+        toma.toma_rms_norm_q8(x, None, x.to(F8), torch.zeros(4, dtype=torch.float64, device="cuda"))
+
+
+@pytest.mark.gpu
+def test_results_are_the_same_every_time(toma):
+    g = generator(13)
+    for m, n, k in ((2, 640, 5120), (100, 640, 5120), (600, 1280, 2560), (3000, 640, 640)):
+        a, w, r = rand(g, m, k, dtype=BF16), rand(g, k, n, dtype=BF16), rand(g, m, n, dtype=BF16)
+        for t in ((a, w, r), (a.float(), w.float(), r.float())):
+            first = torch.empty_like(t[2])
+            toma.toma_linear_act(t[0], t[1], first, act="gelu", residual=t[2])
+            for _ in range(5):
+                c = torch.full_like(t[2], float("nan"))
+                toma.toma_linear_act(t[0], t[1], c, act="gelu", residual=t[2])
+                assert torch.equal(c, first)
 
 
 # ---- the layer, and a run of the operators together ----
