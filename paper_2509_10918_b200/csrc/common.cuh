@@ -147,13 +147,6 @@ struct LinearPlusOp {
   void* c;
   int lda, ldw, ldr, ldc, act;
 };
-// What a device holds at once: SMs, pairs, and clusters of 2, 4, 8 CTAs and of 2, 3 pairs that split a contraction.
-struct PlusDevice {
-  int sms, pairs, split[3], pair_split[2];
-};
-// The form it takes on the tensor cores: 128 x 128 (4), 128 x 192 (2), 256 x 256 (3) or 256 x 320 (5) by pairs, or, with the contraction
-// split, 128 x 128 by 2, 4, 8 CTAs (6, 7, 8) or 256 x 256 by 2, 3 pairs (9, 10).  `steps`: of 128 bytes of a row.
-int linear_plus_form(int M, int N, int steps, int act, const PlusDevice& d);
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
 // At most 16 rows (fp32: of 16-byte packets).
 cudaError_t launch_linear_rows(const LinearPlusOp& o, bool f32, cudaStream_t s);

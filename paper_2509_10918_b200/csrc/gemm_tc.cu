@@ -13,6 +13,7 @@
 // C = act(A W + bias) + residual (launch_linear_plus_tc) runs on the same kernels, with A and W in bf16 or in e4m3 (A with a
 // scale for each row, W stored [n][k] with a scale for each column): kPlus and kPlus8 below.
 #include <climits>
+#include <mutex>
 
 #include "clusters.cuh"
 #include "common.cuh"
@@ -987,51 +988,24 @@ cudaError_t launch_linear_tc(int M, int N, int K, const void* a, const void* con
 }
 
 namespace {
-template <int kKind>
-cudaError_t run_plus(const LinearPlusOp& o, const CUtensorMap& ta, const CUtensorMap& tw, const LinearPlus& plus, uint32_t* dev_status, cudaStream_t s) {
-  const int steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
-  const PlusDevice d{sm_count(),
-                     pairs_at_once(),
-                     {splits_at_once<kKind, 2>(), splits_at_once<kKind, 4>(), splits_at_once<kKind, 8>()},
-                     {pair_splits_at_once<kKind, 2>(), pair_splits_at_once<kKind, 3>()}};
-  int form = linear_plus_form(o.M, o.N, steps, o.act, d);
-  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 2 && v <= 10) {  // test-only override
-    const bool pair = v == 3 || v == 5, split = v >= 6 && v <= 8;
-    if (pair ? o.M > 128 && d.pairs > 0 : split ? steps >= 1 << (v - 5) && d.split[v - 6] > 0 : v < 9 || (steps >= v - 7 && d.pair_split[v - 9] > 0)) form = v;
-  }
-  switch (form) {
-    case 6: return run_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
-    case 7: return run_split<kKind, 4>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
-    case 8: return run_split<kKind, 8>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
-    case 9: return run_pair_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
-    case 10: return run_pair_split<kKind, 3>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
-    default: break;
-  }
-  CUtensorMap tc, tr = tw;
-  const uint64_t cdims[2] = {(uint64_t)o.N, (uint64_t)o.M}, cstr[1] = {(uint64_t)o.ldc * 2}, rstr[1] = {(uint64_t)o.ldr * 2};
-  const uint32_t cbox[2] = {64, 32};  // a warp's 32 rows of one 64-column slab
-  if (!encode_tmap_16bit(&tc, o.c, 2, cdims, cstr, cbox) || (o.residual && !encode_tmap_16bit(&tr, o.residual, 2, cdims, rstr, cbox)))
-    return cudaErrorInvalidValue;
-  CUtensorMap th = tw;
-  if (form == 5) {  // half slabs of W
-    const uint64_t wdims[2] = {(uint64_t)(o.f8 ? o.K : o.N), (uint64_t)(o.f8 ? o.N : o.K)}, wstr[1] = {(uint64_t)o.ldw * (o.f8 ? 1 : 2)};
-    const uint32_t hbox[2] = {o.f8 ? 128u : 32u, o.f8 ? 32u : 64u};
-    if (!(o.f8 ? encode_tmap_8bit : encode_tmap_16bit)(&th, o.w, 2, wdims, wstr, hbox)) return cudaErrorInvalidValue;
-  }
-  const CUtensorMap tws[3] = {tw, tr, th}, tcs[3] = {tc, tc, tc};
-  return run_form<kKind>(form, d.pairs, o.M, o.N, o.K, 1, ta, tws, tcs, o.act, plus, dev_status, s);
-}
-}  // namespace
 
-// The form with the least time by this account: rounds of tiles over the SMs, each a fixed part and a part per step (64 contraction
-// elements of bf16, 128 of e4m3), and what is left of a launch.  Nanoseconds, fitted to 266 shapes between 20 x 320 x 1280 and
-// 16384 x 5120 x 1280 in both types, each timed in every form: within 4 to 6 % in the mean (10 to 14 % for the split forms), and the
-// form it names takes 1.02 times as long as the best in the mean.  linear_tc_form()'s choice took 1.15 (3.4 at most: few tiles).
+// What a device holds at once: SMs, pairs, and clusters of 2, 4, 8 CTAs and of 2, 3 pairs that split a contraction.
+struct PlusDevice {
+  int sms, pairs, split[3], pair_split[2];
+};
+// The form of a launch: 128 x 128 (4), 128 x 192 (2), 256 x 256 (3) or 256 x 320 (5) by pairs, or, with the contraction split, 128 x 128 by 2,
+// 4, 8 CTAs (6, 7, 8) or 256 x 256 by 2, 3 pairs (9, 10).  It is the one with the least time by this account: rounds of tiles over
+// the SMs, each a fixed part and a part per step (64 contraction elements of bf16, 128 of e4m3), and what is left of a launch.
+// Nanoseconds, fitted to 266 shapes between 20 x 320 x 1280 and 16384 x 5120 x 1280 in both types, each timed in every form: within 4
+// to 6 % in the mean (10 to 14 % for the split forms), and the form it names takes 1.02 times as long as the best in the mean;
+// linear_tc_form()'s choice took 1.15 times as long (3.4 at most: few tiles).  Timed too and never the best by more than 2 %: 128 x 256,
+// 256 x 128 by pairs, 256 x 256 by 4 pairs; 256 x 512 by pairs, one accumulator, was slower everywhere (16384 x 5120 x 1280 in 8 bits 106 us
+// against 91).
 // The forms of 256 rows are for more than 128.  An activation is hidden under the next tile's steps but for the form that has one
 // accumulator.
-int linear_plus_form(int M, int N, int steps, int act, const PlusDevice& d) {
+int plus_form(int M, int N, int steps, int act, const PlusDevice& d) {
   const auto tiles = [&](int rows, int cols) { return (long long)((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
-  int best = 0;
+  int best = 4;
   long long least = LLONG_MAX;
   const auto offer = [&](int form, long long count, int at_once, int parts, int launch, int round, int step) {
     if (at_once < 1 || steps < parts) return;
@@ -1049,19 +1023,71 @@ int linear_plus_form(int M, int N, int steps, int act, const PlusDevice& d) {
   return best;
 }
 
+template <int kKind>
+cudaError_t run_plus(const LinearPlusOp& o, int form, const PlusDevice& d, uint32_t* dev_status, cudaStream_t s) {
+  constexpr bool f8 = kKind == kPlus8;
+  constexpr auto encode = f8 ? encode_tmap_8bit : encode_tmap_16bit;
+  CUtensorMap ta, tw;
+  const uint64_t adims[2] = {(uint64_t)o.K, (uint64_t)o.M}, astr[1] = {(uint64_t)o.lda * (f8 ? 1 : 2)};
+  const uint32_t abox[2] = {f8 ? 128u : 64u, 128};
+  const uint64_t wdims[2] = {(uint64_t)(f8 ? o.K : o.N), (uint64_t)(f8 ? o.N : o.K)}, wstr[1] = {(uint64_t)o.ldw * (f8 ? 1 : 2)};
+  const uint32_t wbox[2] = {f8 ? 128u : 64u, 64};
+  if (!encode(&ta, o.a, 2, adims, astr, abox) || !encode(&tw, o.w, 2, wdims, wstr, wbox)) return cudaErrorInvalidValue;
+  const LinearPlus plus{(const __nv_bfloat16*)o.bias, (const __nv_bfloat16*)o.residual, o.a_scale, o.w_scale, (__nv_bfloat16*)o.c, o.ldc, o.ldr};
+  switch (form) {
+    case 6: return run_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 7: return run_split<kKind, 4>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 8: return run_split<kKind, 8>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 9: return run_pair_split<kKind, 2>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    case 10: return run_pair_split<kKind, 3>(o.M, o.N, o.K, ta, tw, o.act, plus, dev_status, s);
+    default: break;
+  }
+  CUtensorMap tc, tr = tw, th = tw;
+  const uint64_t cdims[2] = {(uint64_t)o.N, (uint64_t)o.M}, cstr[1] = {(uint64_t)o.ldc * 2}, rstr[1] = {(uint64_t)o.ldr * 2};
+  const uint32_t cbox[2] = {64, 32};  // a warp's 32 rows of one 64-column slab
+  const uint32_t hbox[2] = {f8 ? 128u : 32u, f8 ? 32u : 64u};  // half a slab of W
+  if (!encode_tmap_16bit(&tc, o.c, 2, cdims, cstr, cbox) || (o.residual && !encode_tmap_16bit(&tr, o.residual, 2, cdims, rstr, cbox)) ||
+      (form == 5 && !encode(&th, o.w, 2, wdims, wstr, hbox)))
+    return cudaErrorInvalidValue;
+  const CUtensorMap tws[3] = {tw, tr, th}, tcs[3] = {tc, tc, tc};
+  return run_form<kKind>(form, d.pairs, o.M, o.N, o.K, 1, ta, tws, tcs, o.act, plus, dev_status, s);
+}
+
+template <int kKind>
+PlusDevice plus_device() {  // (asked once per device)
+  static std::once_flag once[64];
+  static PlusDevice known[64];
+  const auto ask = [] {
+    return PlusDevice{sm_count(),
+                      pairs_at_once(),
+                      {splits_at_once<kKind, 2>(), splits_at_once<kKind, 4>(), splits_at_once<kKind, 8>()},
+                      {pair_splits_at_once<kKind, 2>(), pair_splits_at_once<kKind, 3>()}};
+  };
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ask();
+  std::call_once(once[dev], [&] { known[dev] = ask(); });
+  return known[dev];
+}
+
+template <int kKind>
+cudaError_t launch_plus(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
+  const int steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
+  const PlusDevice d = plus_device<kKind>();
+  int form = plus_form(o.M, o.N, steps, o.act, d);
+  if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 2 && v <= 10) {  // test-only override
+    const bool pair = v == 3 || v == 5, split = v >= 6 && v <= 8;
+    if (pair ? o.M > 128 && d.pairs > 0 : split ? steps >= 1 << (v - 5) && d.split[v - 6] > 0 : v < 9 || (steps >= v - 7 && d.pair_split[v - 9] > 0)) form = v;
+  }
+  return run_plus<kKind>(o, form, d, dev_status, s);
+}
+
+}  // namespace
+
 // c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
   const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
   if (o.M <= 16 && (tune == 0 || tune == 1)) return launch_linear_rows(o, false, s);
-  CUtensorMap ta, tw;
-  const uint64_t adims[2] = {(uint64_t)o.K, (uint64_t)o.M}, astr[1] = {(uint64_t)o.lda * (o.f8 ? 1 : 2)};
-  const uint32_t abox[2] = {o.f8 ? 128u : 64u, 128};
-  const uint64_t wdims[2] = {(uint64_t)(o.f8 ? o.K : o.N), (uint64_t)(o.f8 ? o.N : o.K)}, wstr[1] = {(uint64_t)o.ldw * (o.f8 ? 1 : 2)};
-  const uint32_t wbox[2] = {o.f8 ? 128u : 64u, 64};
-  const auto encode = o.f8 ? encode_tmap_8bit : encode_tmap_16bit;
-  if (!encode(&ta, o.a, 2, adims, astr, abox) || !encode(&tw, o.w, 2, wdims, wstr, wbox)) return cudaErrorInvalidValue;
-  const LinearPlus plus{(const __nv_bfloat16*)o.bias, (const __nv_bfloat16*)o.residual, o.a_scale, o.w_scale, (__nv_bfloat16*)o.c, o.ldc, o.ldr};
-  return o.f8 ? run_plus<kPlus8>(o, ta, tw, plus, dev_status, s) : run_plus<kPlus>(o, ta, tw, plus, dev_status, s);
+  return o.f8 ? launch_plus<kPlus8>(o, dev_status, s) : launch_plus<kPlus>(o, dev_status, s);
 }
 
 }  // namespace toma
