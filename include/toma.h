@@ -12,7 +12,7 @@
  *
  * Conventions that hold for every entry point
  *   - Every data pointer is DEVICE memory owned by the caller, 16-byte aligned,
- *     dense row-major.  `desc` is HOST memory.  The library never allocates,
+ *     dense row-major (rows may be strided where an entry point takes ld*).  `desc` is HOST memory.  The library never allocates,
  *     frees or synchronises; work is enqueued on `stream` (a cudaStream_t
  *     passed as void*; NULL is the default stream).
  *   - Errors the host can detect (null pointers, shapes that do not divide,
@@ -255,7 +255,9 @@ TOMA_API toma_status toma_rms_norm_q8(int32_t rows, int32_t dim, const void* x, 
 
 /* Projection with its epilogue: c = act(a w + bias) + residual, rounded once to dtype (sums and epilogue in fp32).
  *   a [m][k], w [k][n] (dense), c [m][n]; bias [n] or NULL; residual [m][n] or NULL; act: a toma_act.
- *   bf16 needs n and k multiples of 8 and runs on the tensor cores; fp32 takes any, on FFMA.
+ *   bf16 needs n and k multiples of 8 and runs on the tensor cores.  fp32 takes any n and k: on the tensor cores as sums of three
+ *   bf16 numbers where n, k and the strides are multiples of 4 and there are more than 16 rows (as exact as a sum in fp32, but for
+ *   elements below 2^-100, which may lose their last bits), else on FFMA.
  *   Allowed: c = residual (same address and stride). */
 TOMA_API toma_status toma_linear_act(int32_t m, int32_t n, int32_t k, int32_t dtype, const void* a, int32_t lda, const void* w, const void* bias,
                                      int32_t act, const void* residual, int32_t ldr, void* c, int32_t ldc, uint32_t* dev_status, void* stream);

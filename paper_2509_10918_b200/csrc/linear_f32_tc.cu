@@ -1,11 +1,12 @@
 // c = act(a w + bias) + residual in fp32 on the tensor cores, for more than 16 rows.
 //
 // A float is the sum of three bf16 numbers, exactly: x = x0 + x1 + x2 with x0 = bf16(x), x1 = bf16(x - x0), x2 = x - x0 - x1 (8 bits
-// each of the 24).  Of the nine products of two such sums the three smallest are below 2^-25 of the whole, the other six are
+// each of the 24).  Of the nine products of two such sums three are left out (two of at most 2^-25 of the whole, one of 2^-34), the other six are
 // multiplied by tcgen05, whose products are exact and whose sums are in fp32.  A long chain of such sums is not as exact as one of
 // fused multiply-adds (they are cut off, not rounded), so a chain ends after 128 contraction elements, the five small products have one
-// of their own, and the chains' sums are added up by the threads, rounded: 512 x 256 x 640 is 1.6 units of 2^-24 off 64 bits
-// (root mean square), 7.6 on FFMA.  Six bf16 products run at some 375 TFLOP/s, FFMA at 75.
+// of their own, and the chains' sums are added up by the threads, rounded: 512 x 256 x 640 is 2.0 units of 2^-24 off 64 bits
+// (root mean square), 7.6 on FFMA; with 4096 contraction elements 2.3 and 19.  At the rate of a large bf16 product six of them make
+// 275 TFLOP/s, FFMA has 75; 2048 x 1152 x 1280 takes 44 us (137 TFLOP/s).
 //
 // A CTA has a tile of 128 x 128 or 128 x 64.  Two groups of eight warps take the floats of every second stage of 32 contraction elements from
 // global memory, the group's next stage in registers meanwhile, and cut them into three planes each in shared memory (four

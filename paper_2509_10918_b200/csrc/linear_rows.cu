@@ -10,8 +10,8 @@
 //   one of each of eight instructions: columns 8 g + j form instruction j), paired by byte permutations; of a it has 16 bytes.
 //   e4m3, w [n][k]: 64 elements at a time, thread t has elements 16 t .. 16 t + 15, 16 bytes of a column, and of a row of a.
 // The warps' sums are added up through shared memory, the CTAs' through distributed shared memory, in a fixed order.
-// 2 x 5120 x 1280 in bf16 (13 MB of weights, out of L2) 6.9 us, 1 x 640 x 640 3.7, 8-bit 2 x 1280 x 5120 6.0; tiles of 128 rows took 9.5,
-// 6.5 and 14.6.  A launch that does nothing takes 1.9.
+// 2 x 5120 x 1280 in bf16 (13 MB of weights, out of L2) 7.1 us, 1 x 640 x 640 3.7, 8-bit 2 x 1280 x 5120 6.0; tiles of 128 rows took 9.5,
+// 6.5 and 14.6.  A norm of one row of 608, all latency, takes 1.8.
 #include "clusters.cuh"
 #include "linear_epilogue.cuh"
 
