@@ -114,7 +114,8 @@ TOMA_API uint64_t toma_launch_counter(void);
  *   linear_tile    : 1 = 128 x 256, 2 = 128 x 192, 3 = 256 x 256, 4 = 128 x 128 tiles, else heuristic; toma_linear_act and
  *                    toma_linear_q8 in bf16 and e4m3: 1 = the form for at most 16 rows (where there are no more), 2 to 4 the same tiles,
  *                    5 = 256 x 320, 6, 7, 8 = 128 x 128 split by 2, 4, 8 CTAs, 9, 10 = 256 x 256 split by 2, 3 pairs; toma_linear_act
- *                    in fp32 with more than 16 rows: 1, 2 = 128 x 128, 128 x 64, 3, 4 = the first split by 2, 4 CTAs, 5, 6 = the second
+ *                    in fp32 with more than 16 rows: 1, 2 = 128 x 128, 128 x 64, 3, 4 = the first split by 2, 4 CTAs, 5, 6 = the second;
+ *                    all types, at most 16 rows: 11 to 18 = split by 1 to 8 CTAs, 21 to 28 the same of 32 columns (bf16, two rows)
  *   block_unfused  : 1 = toma_block runs merge, attention and unmerge as three kernels even for the shapes its
  *                    one-kernel reuse step covers, selection and weights of 64-token tiles as their separate
  *                    kernels instead of one, and the weights of large tiles through the gather and the logits

@@ -1086,7 +1086,7 @@ cudaError_t launch_plus(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_
 // c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
   const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
-  if (o.M <= 16 && (tune == 0 || tune == 1)) return launch_linear_rows(o, false, s);
+  if (o.M <= 16 && (tune < 2 || tune > 10)) return launch_linear_rows(o, false, s);
   return o.f8 ? launch_plus<kPlus8>(o, dev_status, s) : launch_plus<kPlus>(o, dev_status, s);
 }
 

@@ -97,28 +97,51 @@ __device__ __forceinline__ void add_packet(uint32_t* r, const uint4& b) {
 
 // The epilogue of eight columns of one row, into global memory.
 template <int kKind>
+struct Finish8 {
+  float4 s0, s1;
+  uint4 bias, res;
+  float row_scale;
+  __device__ __forceinline__ void fetch(const LinearPlus& p, int row, int n) {
+    if constexpr (kKind == kPlus8) {
+      s0 = *reinterpret_cast<const float4*>(p.w_scale + n), s1 = *reinterpret_cast<const float4*>(p.w_scale + n + 4);
+      row_scale = p.a_scale[row];
+    }
+    if (p.bias) bias = *reinterpret_cast<const uint4*>(p.bias + n);
+    if (p.residual) res = *reinterpret_cast<const uint4*>(p.residual + (size_t)row * p.ldr + n);
+  }
+  __device__ __forceinline__ void out(float (&v)[8], const LinearPlus& p, int act, __nv_bfloat16* c) const {
+    uint32_t r[8];
+    if constexpr (kKind == kPlus8) {
+      const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= row_scale * s[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(v[e]);
+    if (p.bias) add_packet(r, bias);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      if (act == kActGelu) gelu2(r[e], r[e + 1]);
+      else if (act == kActSilu) by_sigmoid2<kActSilu>(r[e], r[e + 1]);
+      else if (act == kActGeluTanh) by_sigmoid2<kActGeluTanh>(r[e], r[e + 1]);
+    }
+    if (p.residual) add_packet(r, res);
+    __align__(16) __nv_bfloat162 q[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1]));
+    *reinterpret_cast<uint4*>(c) = *reinterpret_cast<const uint4*>(q);
+  }
+};
+template <int kKind>
 __device__ __forceinline__ void finish8(float (&v)[8], float row_scale, const LinearPlus& p, int act, const uint4& res, int n, __nv_bfloat16* c) {
-  uint32_t r[8];
+  Finish8<kKind> f;
   if constexpr (kKind == kPlus8) {
-    const float4 s0 = *reinterpret_cast<const float4*>(p.w_scale + n), s1 = *reinterpret_cast<const float4*>(p.w_scale + n + 4);
-    const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= row_scale * s[e];
+    f.s0 = *reinterpret_cast<const float4*>(p.w_scale + n), f.s1 = *reinterpret_cast<const float4*>(p.w_scale + n + 4);
+    f.row_scale = row_scale;
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(v[e]);
-  if (p.bias) add_packet(r, *reinterpret_cast<const uint4*>(p.bias + n));
-#pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    if (act == kActGelu) gelu2(r[e], r[e + 1]);
-    else if (act == kActSilu) by_sigmoid2<kActSilu>(r[e], r[e + 1]);
-    else if (act == kActGeluTanh) by_sigmoid2<kActGeluTanh>(r[e], r[e + 1]);
-  }
-  if (p.residual) add_packet(r, res);
-  __align__(16) __nv_bfloat162 q[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) q[u] = __floats2bfloat162_rn(__uint_as_float(r[2 * u]), __uint_as_float(r[2 * u + 1]));
-  *reinterpret_cast<uint4*>(c) = *reinterpret_cast<const uint4*>(q);
+  if (p.bias) f.bias = *reinterpret_cast<const uint4*>(p.bias + n);
+  f.res = res;
+  f.out(v, p, act, c);
 }
 
 }  // namespace epi

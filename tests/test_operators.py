@@ -509,6 +509,20 @@ def test_linear_every_tile_form(toma, tuning, tile, m, n, k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("form", [*range(11, 19), *range(21, 29)], ids=[f"{cols}by{split}" for cols in (64, 32) for split in range(1, 9)])
+def test_linear_few_rows_every_split(toma, tuning, form):
+    """Blocks that end inside, contractions shorter than a CTA's steps and none for some, clusters that do not divide a block's eights."""
+    tuning(linear_tile=form)
+    for m, n, k in ((1, 8, 8), (2, 72, 5120), (2, 1288, 648), (1, 5128, 264), (3, 328, 40), (7, 200, 1000), (8, 2568, 136), (16, 1288, 648)):
+        run_linear(toma, m, n, k, BF16, True, "gelu", True, pad=8)
+        run_linear(toma, m, n, k, BF16, False, "none", False, seed=1)
+        run_linear_q8(toma, m, n, k, True, "silu", True, pad=16)
+    for m, n, k in ((1, 4, 4), (2, 68, 5120), (2, 1284, 132), (4, 200, 1000), (7, 324, 60), (16, 1292, 644)):
+        run_linear(toma, m, n, k, F32, True, "gelu_tanh", True, pad=4)
+        run_linear(toma, m, n, k, F32, False, "none", False, seed=1)
+
+
+@pytest.mark.gpu
 def test_linear_in_place_and_side_by_side(toma):
     g = generator(5)
     for m in (2, 100, 1000):
