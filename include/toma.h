@@ -256,7 +256,7 @@ TOMA_API toma_status toma_rms_norm_q8(int32_t rows, int32_t dim, const void* x, 
 
 /* Projection with its epilogue: c = act(a w + bias) + residual, rounded once to dtype (sums and epilogue in fp32).
  *   a [m][k], w [k][n] (dense), c [m][n]; bias [n] or NULL; residual [m][n] or NULL; act: a toma_act.
- *   bf16 needs n and k multiples of 8 and runs on the tensor cores.  fp32 takes any n and k: on the tensor cores as sums of three
+ *   bf16 needs n and k multiples of 8 and runs on the tensor cores (one or two rows: on FFMA).  fp32 takes any n and k: on the tensor cores as sums of three
  *   bf16 numbers where n, k and the strides are multiples of 4 and there are more than 16 rows (as exact as a sum in fp32, but for
  *   elements below 2^-100, which may lose their last bits), else on FFMA.
  *   Allowed: c = residual (same address and stride). */

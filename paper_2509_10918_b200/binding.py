@@ -400,7 +400,7 @@ def _current_device() -> int:
 
 def _act(act) -> int:
     code = ACTIVATIONS.get(act)
-    return code if code is not None else act if isinstance(act, int) else -1
+    return code if code is not None else act if act in (0, 1, 2, 3) else -1
 
 
 def toma_rms_norm(x, weight, y, eps=1e-6, delta=None, sum_out=None):

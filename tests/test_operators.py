@@ -523,6 +523,23 @@ def test_linear_few_rows_every_split(toma, tuning, form):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_linear_few_rows_keep_to_themselves(toma, dtype):
+    """One row with a none-number, one column of w with an infinity: the other rows and columns are what they are without."""
+    g = generator(31)
+    for m in (1, 2, 4, 8, 16):
+        for n, k in ((40, 72), (1288, 648), (5128, 320)):
+            a, w = rand(g, m, k, dtype=dtype), rand(g, k, n, dtype=dtype) / math.sqrt(k)
+            base, c = torch.empty(m, n, dtype=dtype, device="cuda"), torch.empty(m, n, dtype=dtype, device="cuda")
+            toma.toma_linear_act(a, w, base)
+            a[0, k - 1], w[3, n - 1] = float("nan"), float("inf")
+            toma.toma_linear_act(a, w, c)
+            torch.cuda.synchronize()
+            assert torch.isnan(c[0]).all() and not torch.isfinite(c[:, n - 1]).any()
+            assert torch.equal(c[1:, : n - 1], base[1:, : n - 1])
+
+
+@pytest.mark.gpu
 def test_linear_in_place_and_side_by_side(toma):
     g = generator(5)
     for m in (2, 100, 1000):
@@ -625,8 +642,9 @@ def test_binding_refuses_what_it_can_see(toma):
         args.update(bad)
         with pytest.raises(ValueError):
             toma.toma_linear_act(**args)
-    with pytest.raises(toma.TomaError):
-        toma.toma_linear_act(x, w, c, act="relu")
+    for act in ("relu", 4, -1, 2 ** 32 + 1, None):
+        with pytest.raises(toma.TomaError):
+            toma.toma_linear_act(x, w, c, act=act)
     with pytest.raises(toma.TomaError):
         toma.toma_rms_norm(x, None, x, eps=0.0)
     with pytest.raises(ValueError):
