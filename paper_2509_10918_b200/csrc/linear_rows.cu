@@ -13,9 +13,9 @@
 // One or two rows in bf16, and fp32, are multiplied on FFMA (linear_few_kernel, linear_rows_f32_kernel).
 // The warps' sums are added up through shared memory, the CTAs' through distributed shared memory, in a fixed order; bias, scales and
 // residual are on their way meanwhile.
-// 2 rows, weights out of L2 / DRAM in us: bf16 5120 x 1280 4.9 / 6.6, 1280 x 5120 5.5 / 6.8, 5120 x 5120 9.4 / 12.4 (52 MB, 4.2 TB/s), 640 x 640
-// 2.9; e4m3 1280 x 5120 5.6 / 6.0, 5120 x 5120 10.0 / 12.9; fp32 5120 x 1280 6.4 / 8.1, 10240 x 5120 36.9 (5.7 TB/s).  8 rows: bf16 5120 x 1280
-// 5.5 / 7.1, 5120 x 5120 11.8 / 13.6.  Tiles of 128 rows took 9.5 for 2 x 5120 x 1280, 6.5 for 1 x 640 x 640 and 14.6 for 2 x 1280 x 5120 in e4m3.
+// 2 rows, weights out of L2 / DRAM in us: bf16 5120 x 1280 4.8 / 5.9, 1280 x 5120 5.5 / 6.8, 5120 x 5120 9.4 / 12.4 (52 MB, 4.2 TB/s), 640 x 640
+// 2.9; e4m3 1280 x 5120 5.0 / 5.8, 5120 x 5120 7.7 / 9.8, 10240 x 5120 14.2 / 15.9 (52 MB,
+// 3.3 TB/s); fp32 5120 x 1280 6.4 / 8.1, 10240 x 5120 36.9 (5.7 TB/s).  8 rows: bf16 5120 x 1280 6.0 / 7.1, 5120 x 5120 11.7 / 13.6.  Tiles of 128 rows took 9.5 for 2 x 5120 x 1280, 6.5 for 1 x 640 x 640 and 14.6 for 2 x 1280 x 5120 in e4m3.
 // A norm of one row of 608, all latency, takes 1.8.
 #include <climits>
 #include <mutex>
@@ -106,14 +106,21 @@ struct Step {
   uint4 w[8], a[kTall ? 2 : 1];
   __device__ __forceinline__ void load(const RowsOp& o, int step, int n0, int g, int t, bool there) {
     if constexpr (kKind == kPlus8) {
-      const int k = step * 64 + 16 * t, left = there ? o.K - k : 0;
+      const int k = step * 64 + 16 * t, cols = o.N - n0 - g;
+      const uint8_t* w_at = (const uint8_t*)o.w + (size_t)(n0 + g) * o.ldw + k;
+      const uint8_t* a_at = (const uint8_t*)o.a + (size_t)g * o.lda + k;
+      if (there && step * 64 + 64 <= o.K) {  // (a step's end inside a packet is tested for once, not for each)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int n = n0 + 8 * j + g;
-        w[j] = load16_e4m3((const uint8_t*)o.w + (size_t)n * o.ldw + k, n < o.N ? left : 0);
+        for (int j = 0; j < 8; ++j, w_at += 8 * o.ldw) w[j] = 8 * j < cols ? load16(w_at) : none16();
+#pragma unroll
+        for (int i = 0; i < (kTall ? 2 : 1); ++i, a_at += (size_t)8 * o.lda) a[i] = g + 8 * i < o.M ? load16(a_at) : none16();
+      } else {
+        const int left = there ? o.K - k : 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j, w_at += 8 * o.ldw) w[j] = load16_e4m3(w_at, 8 * j < cols ? left : 0);
+#pragma unroll
+        for (int i = 0; i < (kTall ? 2 : 1); ++i, a_at += (size_t)8 * o.lda) a[i] = load16_e4m3(a_at, g + 8 * i < o.M ? left : 0);
       }
-#pragma unroll
-      for (int i = 0; i < (kTall ? 2 : 1); ++i) a[i] = load16_e4m3((const uint8_t*)o.a + (size_t)(g + 8 * i) * o.lda + k, g + 8 * i < o.M ? left : 0);
     } else {
       const int k = step * 32 + 8 * t;
       const bool in_k = there && k < o.K;
@@ -338,13 +345,15 @@ __global__ void __launch_bounds__(kWarps * 32, kRows > 8 ? 1 : 2) linear_rows_f3
 }
 
 // How many CTAs split a block's contraction, and the time that it then takes beside what all have in common: what a cluster costs, and a
-// part for each step in the longest chain of them, which is longer where an SM has two CTAs.  In nanoseconds, fitted for each kernel
-// (RowsCost) to blocks of 40 matrices between 320 x 320 and 5120 x 10240 split by 1 to 8, with the weights in L2 and in DRAM: the split it
-// names takes 1.01 to 1.04 times as long as the best in the mean, 1.24 at most.  More CTAs than the device has places for (two per
-// SM, fewer for clusters: 33 of eight) are what costs most, 3.5 us for 2 x 5120 x 320 in clusters of four; powers of two up to two
-// CTAs per SM, the rule before, had 2 x 5120 x 1280 take 7.0 us, now 4.8, and 2 x 5120 x 640 5.4, now 3.6.
+// part for each step in the longest chain of them (one at least), which is longer where an SM has two CTAs.  In nanoseconds, fitted for
+// each kernel (RowsCost) to blocks of 48 matrices between 320 x 200 and 10240 x 5120 split by 1 to 8, with the weights in L2 and in DRAM: the
+// split it names takes 1.01 to 1.03 times as long as the best in the mean, 1.21 at most.  More CTAs than the device has places for (two per
+// SM, fewer for clusters: 33 of eight) are what costs most, 3.5 us for 2 x 5120 x 320 in clusters of four
+// (counted as 7, which keeps 2 x 10240 x 5120 in bf16 out of it, 22 us in one round and 24 from DRAM in two, and leaves it to fp32, 39 and
+// 37); powers of two up to two
+// CTAs per SM, the rule before, had 2 x 5120 x 1280 take 7.0 us, now 4.8, and 2 x 5120 x 640 5.4, now 3.7.
 struct RowsCost {
-  int cluster, one, two, chains;  // ..., a step with one CTA on an SM, with two, chains of steps in a CTA
+  int cluster, one, two, both, chains;  // ..., a step with one CTA on an SM, with two, what two have besides, chains of steps in a CTA
 };
 struct RowsSplit {
   int split;
@@ -371,8 +380,9 @@ RowsSplit split_of(Kernel kernel, RowsDevice& known, int blocks, int steps, cons
     if (at_once < 1) continue;
     const int rounds = (blocks + at_once - 1) / at_once;
     const bool both = 2LL * blocks > at_once && at_once * split > known.sms[dev];  // two CTAs on an SM
-    const long long round = (split > 1 ? c.cluster : 0) + (both ? 600 : 0) + (long long)steps * (both ? c.two : c.one) / (c.chains * split);
-    const long long cost = split == asked ? 0 : rounds * round + (rounds - 1) * (split > 1 ? 5000 : 0);
+    const long long step = both ? c.two : c.one, chain = steps * step / (c.chains * split);
+    const long long round = (split > 1 ? c.cluster : 0) + (both ? c.both : 0) + (chain > step ? chain : step);
+    const long long cost = split == asked ? 0 : rounds * round + (rounds - 1) * (split > 1 ? 7000 : 0);
     if (cost < best.cost) best = RowsSplit{split, cost};
   }
   return best;
@@ -400,7 +410,7 @@ template <int kCols>
 RowsSplit few_split(const LinearPlusOp& l) {
   static RowsDevice st;
   constexpr int kStepK = 2048 / kCols;
-  return split_of(linear_few_kernel<kCols>, st, (l.N + kCols - 1) / kCols, (l.K + kStepK - 1) / kStepK, RowsCost{870, 580, 1050, kWarps});
+  return split_of(linear_few_kernel<kCols>, st, (l.N + kCols - 1) / kCols, (l.K + kStepK - 1) / kStepK, RowsCost{690, 630, 1240, 100, kWarps});
 }
 template <int kCols>
 cudaError_t run_few(const LinearPlusOp& l, const LinearPlus& plus, int split, cudaStream_t s) {
@@ -421,17 +431,17 @@ cudaError_t run_few(const LinearPlusOp& l, const LinearPlus& plus, cudaStream_t 
 cudaError_t launch_linear_rows(const LinearPlusOp& l, bool f32, cudaStream_t s) {
   cudaError_t e;
   if (f32) {
-    e = l.M > 8   ? run_rows_f32<16>(l, RowsCost{1320, 900, 900, 1}, s)
-        : l.M > 4 ? run_rows_f32<8>(l, RowsCost{1390, 550, 950, 1}, s)
-        : l.M > 2 ? run_rows_f32<4>(l, RowsCost{1200, 380, 640, 1}, s)
-                  : run_rows_f32<2>(l, RowsCost{1080, 285, 470, 1}, s);
+    e = l.M > 8   ? run_rows_f32<16>(l, RowsCost{1360, 895, 895, 0, 1}, s)
+        : l.M > 4 ? run_rows_f32<8>(l, RowsCost{1320, 550, 925, 1340, 1}, s)
+        : l.M > 2 ? run_rows_f32<4>(l, RowsCost{1160, 370, 580, 860, 1}, s)
+                  : run_rows_f32<2>(l, RowsCost{1010, 280, 466, 820, 1}, s);
   } else {
     const LinearPlus plus{(const __nv_bfloat16*)l.bias, (const __nv_bfloat16*)l.residual, l.a_scale, l.w_scale, (__nv_bfloat16*)l.c, l.ldc, l.ldr};
     if (l.f8)
-      e = l.M > 8 ? run_rows<kPlus8, true>(l, plus, RowsCost{1660, 1570, 2230, kWarps}, s) : run_rows<kPlus8, false>(l, plus, RowsCost{1350, 1160, 1830, kWarps}, s);
+      e = l.M > 8 ? run_rows<kPlus8, true>(l, plus, RowsCost{1300, 1300, 2280, 90, kWarps}, s) : run_rows<kPlus8, false>(l, plus, RowsCost{920, 850, 1620, 0, kWarps}, s);
     else
-      e = l.M > 8   ? run_rows<kPlus, true>(l, plus, RowsCost{1390, 850, 1470, kWarps}, s)
-          : l.M > 2 ? run_rows<kPlus, false>(l, plus, RowsCost{960, 730, 1370, kWarps}, s)
+      e = l.M > 8   ? run_rows<kPlus, true>(l, plus, RowsCost{1150, 900, 1680, 320, kWarps}, s)
+          : l.M > 2 ? run_rows<kPlus, false>(l, plus, RowsCost{800, 780, 1590, 0, kWarps}, s)
                     : run_few(l, plus, s);
   }
   count_launch();
