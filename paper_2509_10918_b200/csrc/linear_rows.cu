@@ -111,13 +111,13 @@ struct Step {
       const uint8_t* a_at = (const uint8_t*)o.a + (size_t)g * o.lda + k;
       if (there && step * 64 + 64 <= o.K) {  // (a step's end inside a packet is tested for once, not for each)
 #pragma unroll
-        for (int j = 0; j < 8; ++j, w_at += 8 * o.ldw) w[j] = 8 * j < cols ? load16(w_at) : none16();
+        for (int j = 0; j < 8; ++j, w_at += (size_t)8 * o.ldw) w[j] = 8 * j < cols ? load16(w_at) : none16();
 #pragma unroll
         for (int i = 0; i < (kTall ? 2 : 1); ++i, a_at += (size_t)8 * o.lda) a[i] = g + 8 * i < o.M ? load16(a_at) : none16();
       } else {
         const int left = there ? o.K - k : 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j, w_at += 8 * o.ldw) w[j] = load16_e4m3(w_at, 8 * j < cols ? left : 0);
+        for (int j = 0; j < 8; ++j, w_at += (size_t)8 * o.ldw) w[j] = load16_e4m3(w_at, 8 * j < cols ? left : 0);
 #pragma unroll
         for (int i = 0; i < (kTall ? 2 : 1); ++i, a_at += (size_t)8 * o.lda) a[i] = load16_e4m3(a_at, g + 8 * i < o.M ? left : 0);
       }
