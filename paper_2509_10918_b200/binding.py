@@ -342,6 +342,7 @@ def toma_mlp(rows, dim, hidden, dtype, x, w1, w2, out, ws, dev_status=None):
 
 _BF16, _F32, _E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
 _LD_UNIT = {_BF16: 8, _F32: 4, _E4M3: 16}
+_INT32 = 2 ** 31 - 1  # what the library takes: ctypes keeps the low 32 bits of a larger number without a word
 
 
 def _refuse(t, name, dtype, shape, device):
@@ -364,6 +365,8 @@ def _rows(t, name, dtype, shape, device):
     if shape[0] == 1:  # the stride of a single row is no one's
         unit = _LD_UNIT[dtype]
         ld = (shape[1] + unit - 1) // unit * unit
+    elif ld > _INT32:
+        raise ValueError(f"{name}: rows {ld} elements apart, at most {_INT32} are taken")
     return t.data_ptr(), ld
 
 
@@ -380,6 +383,8 @@ def _shape2(t, name):
     shape = t.shape
     if len(shape) != 2:
         raise ValueError(f"{name}: expected a matrix, got {list(shape)}")
+    if shape[0] > _INT32 or shape[1] > _INT32:
+        raise ValueError(f"{name}: at most {_INT32} rows and columns are taken, got {list(shape)}")
     return shape
 
 
@@ -469,6 +474,8 @@ def toma_quantise_weight(w, q, scale):
 
 
 def toma_mlp_layer_workspace_bytes(rows, dim, hidden, dtype) -> int:
+    if max(rows, dim, hidden) > _INT32:
+        raise ValueError(f"at most {_INT32} rows, channels and hidden channels are taken, got {rows}, {dim}, {hidden}")
     return int(lib.toma_mlp_layer_workspace_bytes(rows, dim, hidden, _dtype_code(dtype)))
 
 

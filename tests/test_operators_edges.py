@@ -51,3 +51,75 @@ def test_few_rows_far_apart(toma, m):  # noqa: F811
     toma.toma_linear_q8(a, a_scale, w, w_scale, c)
     torch.cuda.synchronize()
     assert_linear(c, a.float(), w.float().t(), a_scale=a_scale, w_scale=w_scale)
+
+
+# ---- what a call cannot carry: sizes and strides beyond 32 bits ----
+
+def meta(shape, stride, dtype):
+    return torch.empty_strided(shape, stride, dtype=dtype, device="meta")
+
+
+@pytest.fixture
+def no_device(toma, monkeypatch):  # noqa: F811
+    """The binding with tensors that have no memory taken for the current device's: what it refuses, it refuses before the library's
+    call, which fails the test."""
+    from paper_2509_10918_b200 import binding
+
+    def called(*args):
+        raise AssertionError("reached the library")
+
+    at = meta((1,), (1,), BF16).get_device()
+    monkeypatch.setattr(binding, "_current_device", lambda: at)
+    for name in ("toma_rms_norm", "toma_rms_norm_q8", "toma_linear_act", "toma_linear_q8", "toma_quantise_weight", "toma_mlp_layer"):
+        monkeypatch.setattr(binding.lib, name, called)
+    monkeypatch.setattr(binding, "_stream", lambda: None)
+    return binding
+
+
+FAR = [2 ** 31, 2 ** 32 + 64, 2 ** 33]
+
+
+@pytest.mark.parametrize("far", FAR)
+def test_strides_beyond_32_bits_are_refused(no_device, far):
+    b = no_device
+    f32, one = torch.float32, meta((64,), (1,), BF16)
+    x, wide = meta((2, 64), (64, 1), BF16), meta((2, 64), (far, 1), BF16)
+    q, q_wide, scale = meta((2, 64), (64, 1), F8), meta((2, 64), (far, 1), F8), meta((2,), (1,), f32)
+    w = meta((64, 64), (64, 1), BF16)
+    w8, w8_wide, scales = meta((64, 64), (64, 1), F8), meta((64, 64), (far, 1), F8), meta((64,), (1,), f32)
+    for call in (
+            lambda: b.toma_rms_norm(wide, one, x), lambda: b.toma_rms_norm(x, one, wide), lambda: b.toma_rms_norm(x, one, x, delta=wide),
+            lambda: b.toma_rms_norm(x, one, x, delta=x, sum_out=wide), lambda: b.toma_rms_norm_q8(x, one, q_wide, scale),
+            lambda: b.toma_rms_norm_q8(wide, one, q, scale), lambda: b.toma_linear_act(wide, w, x), lambda: b.toma_linear_act(x, w, wide),
+            lambda: b.toma_linear_act(x, w, x, residual=wide), lambda: b.toma_linear_q8(q_wide, scale, w8, scales, x),
+            lambda: b.toma_linear_q8(q, scale, w8_wide, scales, x), lambda: b.toma_linear_q8(q, scale, w8, scales, wide),
+            lambda: b.toma_quantise_weight(w, w8_wide, scales)):
+        with pytest.raises(ValueError, match="apart"):
+            call()
+    with pytest.raises(AssertionError, match="reached"):  # the stride of a single row is no one's
+        b.toma_rms_norm(meta((1, 64), (far, 1), BF16), one, meta((1, 64), (64, 1), BF16))
+
+
+@pytest.mark.parametrize("rows", [2 ** 31, 2 ** 32 + 2])
+def test_sizes_beyond_32_bits_are_refused(no_device, rows):
+    b = no_device
+    x, y = meta((rows, 8), (8, 1), BF16), meta((rows, 8), (8, 1), BF16)
+    q, scale, w8, s8 = meta((rows, 16), (16, 1), F8), meta((rows,), (1,), torch.float32), meta((8, 16), (16, 1), F8), meta((8,), (1,), torch.float32)
+    w, wide = meta((8, 8), (8, 1), BF16), meta((8, rows), (rows, 1), BF16)
+    for call in (lambda: b.toma_rms_norm(x, None, y), lambda: b.toma_rms_norm_q8(x, None, q, scale), lambda: b.toma_linear_act(x, w, y),
+                 lambda: b.toma_linear_act(w, wide, wide), lambda: b.toma_linear_q8(q, scale, w8, s8, y), lambda: b.toma_quantise_weight(wide, q, scale),
+                 lambda: b.toma_mlp_layer_workspace_bytes(rows, 8, 8, "bf16"), lambda: b.toma_mlp_layer_workspace_bytes(8, 8, rows, "f32"),
+                 lambda: b.toma_mlp_layer(x, None, w, None, w, None, y, w), lambda: b.toma_mlp_layer(w, None, wide, None, w, None, w, w)):
+        with pytest.raises(ValueError, match="at most"):
+            call()
+
+
+@pytest.mark.gpu
+def test_rows_more_than_32_bits_apart_are_refused(toma):  # noqa: F811
+    buf = torch.zeros(2 ** 32 + 256, dtype=torch.uint8, device="cuda").view(F8)
+    a, scale = buf.as_strided((2, 64), (2 ** 32 + 64, 1)), torch.ones(2, device="cuda")
+    w, w_scale, c = torch.zeros(64, 64, device="cuda").to(F8), torch.ones(64, device="cuda"), torch.zeros(2, 64, dtype=BF16, device="cuda")
+    with pytest.raises(ValueError):
+        toma.toma_linear_q8(a, scale, w, w_scale, c)
+    with pytest.raises(ValueError):
+        toma.toma_rms_norm_q8(c, None, a, scale)
