@@ -360,7 +360,7 @@ def _rows(t, name, dtype, shape, device):
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         _refuse(t, name, dtype, shape, device)
     ld, step = t.stride()
-    if step != 1:
+    if step != 1 and shape[1] != 1:  # (nor is the step of a single column)
         _refuse(t, name, dtype, shape, device)
     if shape[0] == 1:  # the stride of a single row is no one's
         unit = _LD_UNIT[dtype]

@@ -123,3 +123,25 @@ def test_rows_more_than_32_bits_apart_are_refused(toma):  # noqa: F811
         toma.toma_linear_q8(a, scale, w, w_scale, c)
     with pytest.raises(ValueError):
         toma.toma_rms_norm_q8(c, None, a, scale)
+
+
+# ---- a single column ----
+
+def test_a_single_column_has_no_step(no_device):
+    """[rows, 1] is contiguous whatever the second stride says; a transposed row has the row's length there."""
+    x, w, c = meta((5, 1), (1, 5), torch.float32), meta((1, 1), (1, 1), torch.float32), meta((5, 1), (1, 5), torch.float32)
+    assert x.is_contiguous()
+    with pytest.raises(AssertionError, match="reached"):
+        no_device.toma_linear_act(x, w, c, residual=c)
+    with pytest.raises(ValueError):
+        no_device.toma_linear_act(meta((5, 2), (1, 5), torch.float32), meta((2, 1), (1, 1), torch.float32), c)
+
+
+@pytest.mark.gpu
+def test_single_columns_out_of_rows(toma):  # noqa: F811
+    g = generator(41)
+    for m in (1, 5, 40):
+        a, w, c = rand(g, 1, m).t(), rand(g, 1, 1), torch.empty(1, m, device="cuda").t()
+        toma.toma_linear_act(a, w, c, act="gelu")
+        torch.cuda.synchronize()
+        assert_linear(c, a, w, None, "gelu")
