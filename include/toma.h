@@ -242,14 +242,16 @@ typedef enum {
  *   x, y [rows][dim]; delta [rows][dim] or NULL (h = x); weight [dim] or NULL (ones); sum [rows][dim], where h goes, or NULL
  *   (needs delta, TOMA_ERR_NULL).  dim: a multiple of 8, at most 16384 (TOMA_ERR_UNSUPPORTED).  eps > 0.
  *   Allowed: sum = x, sum = delta, y = x or y = delta (same address and stride).
- * The mean is held in fp32 and overflows for magnitudes above about 1e18.  No waits, so no dev_status. */
+ * The sum of squares is held in fp32.  It overflows where a row's root mean square is above sqrt(3.4e38 / dim) (2.3e18 at dim 64, 7.3e17 at
+ * 640, 1.4e17 at 16384), and such a row has y = 0.  No waits, so no dev_status. */
 TOMA_API toma_status toma_rms_norm(int32_t rows, int32_t dim, int32_t dtype, const void* x, int32_t ldx, const void* delta, int32_t ldd,
                                    const void* weight, float eps, void* sum, int32_t lds, void* y, int32_t ldy, void* stream);
 
 /* The same in bf16 with y in 8 bits: q [rows][dim] e4m3 and scale [rows] fp32 with y ~ q * scale.  With p = h * weight,
  *   q = e4m3(448 p / max|p|), to nearest, ties to even, decided without rounding in between, and
  *   scale = max|p| / (448 sqrt(mean(h^2) + eps)).
- * A row whose max|p| is below 2^-100 has q = 0 and scale = 0; one with an infinity or a NaN has NaN throughout, scale too.
+ * A row whose max|p| is below 2^-100 has q = 0 and scale = 0; one with an infinity or a NaN among h or p has NaN throughout, scale too.
+ * One whose sum of squares overflows has scale = 0.
  * Allowed: sum = x, sum = delta.  ldq: a multiple of 16. */
 TOMA_API toma_status toma_rms_norm_q8(int32_t rows, int32_t dim, const void* x, int32_t ldx, const void* delta, int32_t ldd, const void* weight,
                                       float eps, void* sum, int32_t lds, void* q, int32_t ldq, float* scale, void* stream);

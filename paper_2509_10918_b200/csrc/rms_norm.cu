@@ -2,7 +2,7 @@
 // y = h / sqrt(mean(h^2) + eps) * weight, in the tensors' type or in e4m3 with a scale for each row.
 //
 // One pass: a row's elements stay in the registers of the threads that loaded them, between the loads and the stores there is
-// the sum of their squares (fp32: chains of at most 40 terms, then a tree) and for 8 bits the maximum of |h weight|.
+// the sum of their squares (fp32: two chains of at most 20 terms a thread, then a tree) and for 8 bits the maximum of |h weight|.
 // 8 bits: q = e4m3(448 p / max|p|) with p = h weight, which bf16 factors give exactly; 1 / rms is in the row's scale alone.
 //
 // HBM bounds it: 65536 x 640 in bf16 with the addition 53 us (6.3 TB/s), 32767 x 1280 without 27.7 (6.0), to 8 bits 23.7 (5.3, with
@@ -146,7 +146,8 @@ __global__ void __launch_bounds__(kLanes < 256 ? 256 : kLanes, kNormCtas<T, kAdd
     float s0, s1;
     tc::unpack2(ss2, s0, s1);
     const float ss = sum_row<kLanes>(s0 + s1, red_s[turn & 1][group], t);
-    // (what is rounded to 8 or 16 bits or multiplies such: within 2 units of the last place is enough)
+    // (2 units of the last place of rsqrtf: enough for y in 16 bits.  A row's scale in fp32 has them too: 7.3e-8 off, root mean square, where
+    // one rounding of 64 bits is 5.1e-8; below the 2^-4 of the e4m3 that it multiplies in any case.)
     const float r = sizeof(T) == 4 ? 1.f / sqrtf(ss / (float)o.dim + o.eps) : rsqrtf(fmaf(ss, inv_dim, o.eps));
     if constexpr (!kQ8) {
 #pragma unroll

@@ -1,9 +1,11 @@
 """The operators between the blocks at the edges of what they take: far strides, sizes that a call cannot carry, values next to what
 fp32 holds.  Definitions and tolerances as in test_operators.py."""
+import math
+
 import pytest
 import torch
 
-from tests.test_operators import BF16, F8, assert_linear, eight_bits, generator, rand, toma, tuning  # noqa: F401 (fixtures)
+from tests.test_operators import BF16, F8, assert_linear, eight_bits, generator, norm, rand, to_e4m3, toma, tuning  # noqa: F401 (fixtures)
 
 
 @pytest.mark.gpu
@@ -145,3 +147,34 @@ def test_single_columns_out_of_rows(toma):  # noqa: F811
         toma.toma_linear_act(a, w, c, act="gelu")
         torch.cuda.synchronize()
         assert_linear(c, a, w, None, "gelu")
+
+
+# ---- the norm where its sum of squares leaves fp32 ----
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [8, 64, 640, 1280, 5120, 16384])
+def test_norm_next_to_the_overflow_of_its_sum(toma, dim):  # noqa: F811
+    """A row just below sqrt(3.4e38 / dim) is right, one just above is zeros (3 %: bf16 has steps of 0.8 %, the sum errors of 0.1 %)."""
+    bound = math.sqrt(torch.finfo(torch.float32).max / dim)
+    sign = torch.where(rand(generator(dim), dim) < 0, -1.0, 1.0).double()
+    for dtype in (BF16, torch.float32):
+        x = torch.stack([sign * bound * f for f in (0.97, 1.03, 0.5, 1e-3)]).to(dtype)
+        y = torch.empty_like(x)
+        toma.toma_rms_norm(x, None, y)
+        torch.cuda.synchronize()
+        want = norm(x, None, 1e-6)
+        tol = want.abs() * ((2.0 ** -8 if dtype == BF16 else 2.0 ** -24) + 64 * 2.0 ** -24)
+        for r in (0, 2, 3):
+            assert bool(((y[r].double() - want[r]).abs() <= tol[r]).all()), r
+        assert bool((y[1] == 0).all())
+    q, scale = torch.empty(4, (dim + 15) // 16 * 16, dtype=F8, device="cuda")[:, :dim], torch.empty(4, device="cuda")
+    x = x.to(BF16)
+    toma.toma_rms_norm_q8(x, None, q, scale)
+    torch.cuda.synchronize()
+    p = x.double()
+    top = p.abs().amax(1)
+    assert torch.equal(q.double(), to_e4m3(p * 448 / top[:, None]))
+    want = top / 448 / torch.sqrt(p.square().mean(1) + 1e-6)
+    assert float(scale[1]) == 0
+    for r in (0, 2, 3):
+        assert abs(float(scale[r]) - float(want[r])) <= float(want[r]) * 64 * 2.0 ** -24
