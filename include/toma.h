@@ -267,7 +267,8 @@ TOMA_API toma_status toma_linear_act(int32_t m, int32_t n, int32_t k, int32_t dt
 
 /* The same with 8-bit operands: c = act((a w^T)[i][j] a_scale[i] w_scale[j] + bias) + residual.
  *   a [m][k] and w [n][k] e4m3 (w by output column: K innermost, as toma_quantise_weight writes it), a_scale [m] and w_scale [n]
- *   fp32; bias, residual and c bf16.  n and k multiples of 8.  Products are exact, sums and epilogue in fp32. */
+ *   fp32; bias, residual and c bf16.  n and k multiples of 8.  Products are exact, sums and epilogue in fp32 (a sum times a_scale, then
+ *   times w_scale). */
 TOMA_API toma_status toma_linear_q8(int32_t m, int32_t n, int32_t k, const void* a, int32_t lda, const float* a_scale, const void* w, int32_t ldw,
                                     const float* w_scale, const void* bias, int32_t act, const void* residual, int32_t ldr, void* c,
                                     int32_t ldc, uint32_t* dev_status, void* stream);

@@ -173,10 +173,10 @@ struct SlabOut {
       tmem_wait_ld(r);
       const uint64_t rs = both(row_scale);
 #pragma unroll
-      for (int e = 0; e < 32; e += 2) {
-        const uint64_t f = mul2(rs, e % 4 == 0 ? pack2(s[e / 4].x, s[e / 4].y) : pack2(s[e / 4].z, s[e / 4].w));
+      for (int e = 0; e < 32; e += 2) {  // (the row's first: two scales multiplied may leave fp32 where the result does not)
+        const uint64_t f = e % 4 == 0 ? pack2(s[e / 4].x, s[e / 4].y) : pack2(s[e / 4].z, s[e / 4].w);
         float v0, v1;
-        unpack2(mul2(pack2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), f), v0, v1);
+        unpack2(mul2(mul2(pack2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), rs), f), v0, v1);
         r[e] = __float_as_uint(v0);
         r[e + 1] = __float_as_uint(v1);
       }

@@ -114,7 +114,7 @@ struct Finish8 {
     if constexpr (kKind == kPlus8) {
       const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= row_scale * s[e];
+      for (int e = 0; e < 8; ++e) v[e] = v[e] * row_scale * s[e];
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(v[e]);

@@ -178,3 +178,67 @@ def test_norm_next_to_the_overflow_of_its_sum(toma, dim):  # noqa: F811
     assert float(scale[1]) == 0
     for r in (0, 2, 3):
         assert abs(float(scale[r]) - float(want[r])) <= float(want[r]) * 64 * 2.0 ** -24
+
+
+# ---- scales far apart, and operands that are no numbers ----
+
+FORMS = [(2, 0), (12, 0), (40, 0), (300, 0), (300, 2), (300, 3), (300, 4), (300, 5), (300, 6), (300, 7), (300, 9), (300, 10)]  # rows, tile form asked for
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,tile", FORMS)
+def test_q8_scales_whose_product_leaves_fp32(toma, tuning, m, tile):  # noqa: F811
+    """(sum a_scale) w_scale is a number where a_scale w_scale is none (1e45: above fp32; 1e-43: below the normal numbers, 70 units of the
+    least).  The sums are of positive numbers, some 10^7, so that the first product and the result are normal numbers."""
+    tuning(linear_tile=tile)
+    n, k = 328, 640
+    g = generator(m, tile)
+    a, _ = eight_bits(rand(g, m, k).abs() + 1)
+    w, _ = eight_bits(rand(g, n, k).abs() + 1)
+    a[1] = 0
+    c = torch.empty(m, n, dtype=BF16, device="cuda")
+    for sa, sw in ((1e25, 1e20), (1e-23, 1e-20), (1e-31, 1e-12)):
+        a_scale, w_scale = torch.full((m,), sa, device="cuda"), torch.full((n,), sw, device="cuda")
+        if sa > 1:  # only the rows of zeros are numbers there
+            a_scale[0], a_scale[2:] = 1e-30, 1e-30
+        toma.toma_linear_q8(a, a_scale, w, w_scale, c)
+        torch.cuda.synchronize()
+        assert not torch.isnan(c).any() and bool((c[1] == 0).all())
+        assert_linear(c, a.float(), w.float().t(), a_scale=a_scale, w_scale=w_scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,tile", FORMS)
+def test_q8_none_numbers_keep_to_themselves(toma, tuning, m, tile):  # noqa: F811
+    """A none-number in a row of a, in a column of w, in a scale of either, and an infinite scale: the other rows and columns as without."""
+    tuning(linear_tile=tile)
+    n, k = 328, 648
+    g = generator(m, tile, 1)
+    a, a_scale = eight_bits(rand(g, m, k))
+    w, w_scale = eight_bits(rand(g, n, k))
+    clean, c = (torch.empty(m, n, dtype=BF16, device="cuda") for _ in range(2))
+    nan, inf = float("nan"), float("inf")
+    for act in ("none", "gelu", "gelu_tanh", "silu"):
+        toma.toma_linear_q8(a, a_scale, w, w_scale, clean, act=act)
+        for where in ("a", "w", "a_scale", "w_scale"):
+            t = {"a": a.clone(), "w": w.clone(), "a_scale": a_scale.clone(), "w_scale": w_scale.clone()}
+            for name in "aw":  # (rows of whole packets again)
+                padded = torch.zeros(t[name].shape[0], 656, device="cuda").to(F8)[:, :k]
+                padded.copy_(t[name])
+                t[name] = padded
+            at = 1 if where[0] == "a" else n - 3
+            t[where][at if "scale" in where else (at, k - 1)] = nan
+            c.fill_(0)
+            toma.toma_linear_q8(t["a"], t["a_scale"], t["w"], t["w_scale"], c, act=act)
+            torch.cuda.synchronize()
+            bad = torch.zeros_like(c, dtype=torch.bool)
+            if where[0] == "a":
+                bad[at] = True
+            else:
+                bad[:, at] = True
+            assert torch.isnan(c[bad]).all() and torch.equal(c[~bad], clean[~bad]), (act, where)
+        a_inf = a_scale.clone()
+        a_inf[0] = inf
+        toma.toma_linear_q8(a, a_inf, w, w_scale, c, act=act)
+        torch.cuda.synchronize()
+        assert not torch.isfinite(c[0][clean[0].abs() > 1]).any() and torch.equal(c[1:], clean[1:])
