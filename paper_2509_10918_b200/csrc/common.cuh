@@ -148,6 +148,8 @@ struct LinearPlusOp {
   int lda, ldw, ldr, ldc, act;
 };
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s);
+// The form that this takes on the current device, in the test-only numbers of linear_tile.
+int linear_plus_form(int M, int N, int K, bool f8, int act);
 // At most 16 rows (fp32: of 16-byte packets).
 cudaError_t launch_linear_rows(const LinearPlusOp& o, bool f32, cudaStream_t s);
 // fp32: any shape on FFMA; rows of 16-byte packets on the tensor cores.

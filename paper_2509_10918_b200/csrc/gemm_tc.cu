@@ -1069,25 +1069,38 @@ PlusDevice plus_device() {  // (asked once per device)
   return known[dev];
 }
 
+// The form that a launch takes: plus_form()'s, or the test's where the shape and the device allow it.
 template <int kKind>
-cudaError_t launch_plus(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
-  const int steps = (o.K + kStepK<kKind> - 1) / kStepK<kKind>;
-  const PlusDevice d = plus_device<kKind>();
-  int form = plus_form(o.M, o.N, steps, o.act, d);
+int plus_form_of(int M, int N, int K, int act, const PlusDevice& d) {
+  const int steps = (K + kStepK<kKind> - 1) / kStepK<kKind>;
   if (const int v = g_tune_linear_tile.load(std::memory_order_relaxed); v >= 2 && v <= 10) {  // test-only override
     const bool pair = v == 3 || v == 5, split = v >= 6 && v <= 8;
-    if (pair ? o.M > 128 && d.pairs > 0 : split ? steps >= 1 << (v - 5) && d.split[v - 6] > 0 : v < 9 || (steps >= v - 7 && d.pair_split[v - 9] > 0)) form = v;
+    if (pair ? M > 128 && d.pairs > 0 : split ? steps >= 1 << (v - 5) && d.split[v - 6] > 0 : v < 9 || (steps >= v - 7 && d.pair_split[v - 9] > 0)) return v;
   }
-  return run_plus<kKind>(o, form, d, dev_status, s);
+  return plus_form(M, N, steps, act, d);
+}
+bool few_rows(int M) {
+  const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
+  return M <= 16 && (tune < 2 || tune > 10);
+}
+
+template <int kKind>
+cudaError_t launch_plus(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
+  const PlusDevice d = plus_device<kKind>();
+  return run_plus<kKind>(o, plus_form_of<kKind>(o.M, o.N, o.K, o.act, d), d, dev_status, s);
 }
 
 }  // namespace
 
 // c = act(a w + bias) + residual; strides in elements.  bf16: w [K][N].  e4m3 (f8): a and w [N][K] with a_scale [M], w_scale [N].
 cudaError_t launch_linear_plus_tc(const LinearPlusOp& o, uint32_t* dev_status, cudaStream_t s) {
-  const int tune = g_tune_linear_tile.load(std::memory_order_relaxed);  // test-only
-  if (o.M <= 16 && (tune < 2 || tune > 10)) return launch_linear_rows(o, false, s);
+  if (few_rows(o.M)) return launch_linear_rows(o, false, s);
   return o.f8 ? launch_plus<kPlus8>(o, dev_status, s) : launch_plus<kPlus>(o, dev_status, s);
+}
+
+int linear_plus_form(int M, int N, int K, bool f8, int act) {
+  if (few_rows(M)) return 1;
+  return f8 ? plus_form_of<kPlus8>(M, N, K, act, plus_device<kPlus8>()) : plus_form_of<kPlus>(M, N, K, act, plus_device<kPlus>());
 }
 
 }  // namespace toma

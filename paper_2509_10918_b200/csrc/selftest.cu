@@ -38,3 +38,8 @@ extern "C" toma_status toma_test_wait_timeout(uint32_t polls, uint32_t* dev_stat
   toma::count_launch();
   return cudaGetLastError() == cudaSuccess ? TOMA_OK : TOMA_ERR_CUDA;
 }
+
+extern "C" int32_t toma_test_linear_plus_form(int32_t m, int32_t n, int32_t k, int32_t e4m3, int32_t act) {
+  if (!toma::linear_tc_shape_ok(m, n, k) || act < TOMA_ACT_NONE || act > TOMA_ACT_SILU) return 0;
+  return toma::linear_plus_form(m, n, k, e4m3 != 0, act);
+}

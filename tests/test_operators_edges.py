@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from tests.test_operators import BF16, F8, assert_linear, eight_bits, generator, norm, rand, to_e4m3, toma, tuning  # noqa: F401 (fixtures)
+from tests.test_operators import BF16, F8, assert_linear, eight_bits, generator, norm, rand, run_linear, run_linear_q8, to_e4m3, toma, tuning  # noqa: F401 (fixtures)
 
 
 @pytest.mark.gpu
@@ -242,3 +242,39 @@ def test_q8_none_numbers_keep_to_themselves(toma, tuning, m, tile):  # noqa: F81
         toma.toma_linear_q8(a, a_inf, w, w_scale, c, act=act)
         torch.cuda.synchronize()
         assert not torch.isfinite(c[0][clean[0].abs() > 1]).any() and torch.equal(c[1:], clean[1:])
+
+
+# ---- every form, where it is the one that runs ----
+
+TILES = {2: "128x192", 3: "256x256", 4: "128x128", 5: "256x320", 6: "split2", 7: "split4", 8: "split8", 9: "pairs2", 10: "pairs3"}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tile", list(TILES), ids=list(TILES.values()))
+@pytest.mark.parametrize("m,n,k", [(129, 328, 1160), (300, 72, 2056), (257, 1288, 1032), (1000, 648, 1096)])
+def test_the_form_asked_for_runs_over_long_ragged_contractions(toma, tuning, tile, m, n, k):  # noqa: F811
+    """A split by eight has a step for each CTA from 8 on: 1032 elements are 9 steps of e4m3 and 17 of bf16, the last of 8 elements."""
+    tuning(linear_tile=tile)
+    for f8 in (False, True):
+        assert toma.toma_test_linear_plus_form(m, n, k, f8, "gelu") == tile
+    run_linear(toma, m, n, k, BF16, True, "gelu", True, pad=8)
+    run_linear(toma, m, n, k, BF16, False, "none", False, seed=1)
+    run_linear_q8(toma, m, n, k, True, "silu", True, pad=16)
+    run_linear_q8(toma, m, n, k, False, "none", False, seed=1)
+
+
+@pytest.mark.gpu
+def test_forms_by_themselves(toma, tuning):  # noqa: F811
+    """At most 16 rows have their own form, and a form that a shape does not allow is not taken."""
+    form = toma.toma_test_linear_plus_form
+    assert all(form(m, 640, 640, f8) == 1 for m in (1, 16) for f8 in (False, True))
+    assert all(form(m, 640, 640, f8) in TILES for m in (17, 154, 4096) for f8 in (False, True))
+    tuning(linear_tile=8)
+    assert form(300, 640, 448) != 8 and form(300, 640, 456) == 8 and form(300, 640, 896, True) != 8 and form(300, 640, 904, True) == 8
+    tuning(linear_tile=3)
+    assert form(128, 640, 640) != 3 and form(129, 640, 640) == 3
+
+
+def test_forms_of_bad_shapes(toma):  # noqa: F811
+    form = toma.lib.toma_test_linear_plus_form
+    assert form(0, 8, 8, 0, 0) == 0 and form(8, 12, 8, 0, 0) == 0 and form(8, 8, 8, 0, 4) == 0
