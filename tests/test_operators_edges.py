@@ -278,3 +278,31 @@ def test_forms_by_themselves(toma, tuning):  # noqa: F811
 def test_forms_of_bad_shapes(toma):  # noqa: F811
     form = toma.lib.toma_test_linear_plus_form
     assert form(0, 8, 8, 0, 0) == 0 and form(8, 12, 8, 0, 0) == 0 and form(8, 8, 8, 0, 4) == 0
+
+
+# ---- fp32 on the tensor cores: none of the six products missing, chains as short as they are ----
+
+F32_FORMS = ["chosen", "128", "64", "128split2", "128split4", "64split2", "64split4"]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", range(7), ids=F32_FORMS)
+def test_linear_f32_error_does_not_grow_with_the_contraction(toma, tuning, form):  # noqa: F811
+    """The root of the mean square error against 64 bits in units of 2^-24 of the results' root mean square, at most 6 at any length.
+
+    A chain of 128 elements is eight instructions that each add to the sum so far and cut off: 0.5 units of its last place in the mean,
+    a unit being 0.72 2^-23 of it in the mean, the sums on the way 0.66 of the last in the mean: 8 x 0.5 x 0.72 x 0.66 = 1.9 of 2^-23,
+    3.8 of 2^-24 of a chain's sum, towards zero.  Chains' sums have signs of their own, so the errors add up as the sums do: 3.8 of the result
+    at any length.  Adding up k / 128 chains rounds each time, 0.42 of 2^-24 of the sum so far in the root mean square, 0.7 of the
+    last: 0.29 sqrt(k / 128), 2.6 at 10240.  Together 4.6.  One of the six products missing is 40 and more (products of a plane
+    of 2^-16, root mean square), chains that do not end at 128 grow with k.
+    """
+    tuning(linear_tile=form)
+    for m, n, k in ((512, 256, 640), (512, 256, 4096), (130, 200, 1000), (300, 136, 10240)):
+        g = generator(m, n, k, 5)
+        a, w, c = rand(g, m, k), rand(g, k, n), torch.empty(m, n, device="cuda")
+        toma.toma_linear_act(a, w, c)
+        want = a.double() @ w.double()
+        off = float(((c.double() - want).square().mean() / want.square().mean()).sqrt()) * 2 ** 24
+        print(f"f32 {F32_FORMS[form]} {m} x {n} x {k}: {off:.2f} units of 2^-24")
+        assert off <= 6
