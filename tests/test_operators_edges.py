@@ -306,3 +306,30 @@ def test_linear_f32_error_does_not_grow_with_the_contraction(toma, tuning, form)
         off = float(((c.double() - want).square().mean() / want.square().mean()).sqrt()) * 2 ** 24
         print(f"f32 {F32_FORMS[form]} {m} x {n} x {k}: {off:.2f} units of 2^-24")
         assert off <= 6
+
+
+# ---- the layer: the same every time ----
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, torch.float32], ids=["bf16", "f32"])
+def test_layer_repeats_itself(toma, dtype):  # noqa: F811
+    """Whatever its scratch and its result hold before, eager and out of a graph."""
+    for rows, dim, hidden in ((1, 640, 2560), (154, 1280, 5120), (1024, 1280, 5120), (3000, 640, 2560)):
+        g = generator(rows, 3)
+        x, delta, nw = rand(g, rows, dim, dtype=dtype), rand(g, rows, dim, dtype=dtype), rand(g, dim, dtype=dtype)
+        w1, b1 = rand(g, dim, hidden, dtype=dtype) / math.sqrt(dim), rand(g, hidden, dtype=dtype)
+        w2, b2 = rand(g, hidden, dim, dtype=dtype) / math.sqrt(hidden), rand(g, dim, dtype=dtype)
+        ws = torch.empty(toma.toma_mlp_layer_workspace_bytes(rows, dim, hidden, "bf16" if dtype == BF16 else "f32"), dtype=torch.uint8, device="cuda")
+        first, out = torch.empty_like(x), torch.empty_like(x)
+        toma.toma_mlp_layer(x, nw, w1, b1, w2, b2, first, ws, delta=delta)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            toma.toma_mlp_layer(x, nw, w1, b1, w2, b2, out, ws, delta=delta)
+        for i in range(6):
+            out.fill_(float("nan")), ws.fill_(255 if i % 2 else 0)
+            if i < 3:
+                toma.toma_mlp_layer(x, nw, w1, b1, w2, b2, out, ws, delta=delta)
+            else:
+                graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, first)
