@@ -239,6 +239,7 @@ typedef enum {
   TOMA_ACT_GELU_TANH = 2, /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
   TOMA_ACT_SILU = 3       /* v / (1 + exp(-v)) */
 } toma_act;
+/* (v = -infinity, where these have infinity times zero: GELU in bf16 and e4m3 gives its limit 0, all others NaN.) */
 
 /* Root-mean-square norm with the residual's addition, row by row:
  *   h = x + delta, rounded to dtype;  y = h / sqrt(mean(h^2) + eps) * weight, rounded to dtype.

@@ -244,6 +244,34 @@ def test_q8_none_numbers_keep_to_themselves(toma, tuning, m, tile):  # noqa: F81
         assert not torch.isfinite(c[0][clean[0].abs() > 1]).any() and torch.equal(c[1:], clean[1:])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [2, 10, 200])
+def test_activations_of_infinities(toma, m):  # noqa: F811
+    """+infinity stays, and -infinity, where the formulas have infinity times zero, is the limit 0 for GELU in bf16 and NaN elsewhere."""
+    inf = float("inf")
+    for dtype in (BF16, torch.float32):
+        a, w = torch.zeros(m, 16, dtype=dtype, device="cuda"), torch.zeros(16, 32, dtype=dtype, device="cuda")
+        bias, c = torch.zeros(32, dtype=dtype, device="cuda"), torch.empty(m, 32, dtype=dtype, device="cuda")
+        bias[3], bias[20] = inf, -inf
+        for act in ("none", "gelu", "gelu_tanh", "silu"):
+            outs = []
+            toma.toma_linear_act(a, w, c, bias=bias, act=act)
+            outs.append(c.clone())
+            if dtype == BF16:
+                toma.toma_linear_q8(a.to(F8), torch.ones(m, device="cuda"), w.t().contiguous().to(F8), torch.ones(32, device="cuda"), c, bias=bias, act=act)
+                outs.append(c.clone())
+            torch.cuda.synchronize()
+            for out in outs:
+                assert bool((out[:, 3] == inf).all()) and bool((out[:, [0, 19, 21, 31]] == 0).all())
+                low = out[:, 20]
+                if act == "none":
+                    assert bool((low == -inf).all())
+                elif act == "gelu" and dtype == BF16:
+                    assert bool((low == 0).all())
+                else:
+                    assert torch.isnan(low).all()
+
+
 # ---- every form, where it is the one that runs ----
 
 TILES = {2: "128x192", 3: "256x256", 4: "128x128", 5: "256x320", 6: "split2", 7: "split4", 8: "split8", 9: "pairs2", 10: "pairs3"}
