@@ -63,7 +63,7 @@ struct E4m3Row {
 };
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }  // ordered, NaN above infinity
 
-// Eight consecutive elements (16 bytes of bf16, 32 of fp32), aligned to 16 bytes.
+// Eight consecutive elements (16 bytes of bf16, 32 of fp32 in store8), aligned to 16 bytes.
 __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
   const uint4 q = *reinterpret_cast<const uint4*>(p);
   const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -72,10 +72,6 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
     v[2 * e] = __uint_as_float(w[e] << 16);
     v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
   }
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
   __align__(16) __nv_bfloat162 h[4];

@@ -238,8 +238,8 @@ __global__ void __launch_bounds__((kWarps + 1) * 32, 1) linear_f32_kernel(const 
     // An infinity is no sum of three numbers: where one or a none-number has come in, the sums are taken as they are defined, four
     // columns at a time.  (A row with a none-number in it has nothing else, so that rows of padding do not cost their length times the
     // columns.  4096 x 2560 x 2560 takes 0.39 ms, with an infinity in one row 2.3, in one column 2.3, in each row 28; an element at a
-    // time 24, 1.3 and 117.  Eight columns and four rows of w at a time 1.5, 1.1 and 7.4, but the other products 2 to 4 % longer, by the
-    // registers that the compiler then spills.)
+    // time 24, 1.3 and 117.  Eight columns and four rows of w at a time 1.5, 1.1 and 7.4, but all other products 2 to 4 % longer: the forms
+    // of 128 columns have no register left, and spill 104 to 156 bytes as they are.)
     bool odd = false;
 #pragma unroll
     for (int e = 0; e < kPart; ++e) odd |= n_first + e < o.N && !(fabsf(v[e]) < INFINITY);

@@ -13,9 +13,10 @@
 // One or two rows in bf16, and fp32, are multiplied on FFMA (linear_few_kernel, linear_rows_f32_kernel).
 // The warps' sums are added up through shared memory, the CTAs' through distributed shared memory, in a fixed order; bias, scales and
 // residual are on their way meanwhile.
-// 2 rows, weights out of L2 / DRAM in us: bf16 5120 x 1280 4.8 / 5.9, 1280 x 5120 5.5 / 6.8, 5120 x 5120 9.4 / 12.4 (52 MB, 4.2 TB/s), 640 x 640
-// 2.9; e4m3 1280 x 5120 5.0 / 5.8, 5120 x 5120 7.7 / 9.8, 10240 x 5120 14.2 / 15.9 (52 MB,
-// 3.3 TB/s); fp32 5120 x 1280 6.4 / 8.1, 10240 x 5120 36.9 (5.7 TB/s).  8 rows: bf16 5120 x 1280 6.0 / 7.1, 5120 x 5120 11.7 / 13.6.  Tiles of 128 rows took 9.5 for 2 x 5120 x 1280, 6.5 for 1 x 640 x 640 and 14.6 for 2 x 1280 x 5120 in e4m3.
+// In us, weights out of L2 / DRAM.  2 rows in bf16: 5120 x 1280 4.8 / 5.9, 1280 x 5120 5.5 / 6.8, 5120 x 5120 9.4 / 12.4 (52 MB, 4.2 TB/s),
+// 640 x 640 2.9; in e4m3: 1280 x 5120 5.0 / 5.8, 5120 x 5120 7.7 / 9.8, 10240 x 5120 14.2 / 15.9 (52 MB, 3.3 TB/s); in fp32: 5120 x 1280
+// 6.4 / 8.1, 10240 x 5120 36.9 (5.7 TB/s).  8 rows in bf16: 5120 x 1280 6.0 / 7.1, 5120 x 5120 11.7 / 13.6.  Tiles of 128 rows took 9.5 for
+// 2 x 5120 x 1280, 6.5 for 1 x 640 x 640 and 14.6 for 2 x 1280 x 5120 in e4m3.
 // A norm of one row of 608, all latency, takes 1.8.
 #include <climits>
 #include <mutex>
@@ -346,12 +347,11 @@ __global__ void __launch_bounds__(kWarps * 32, kRows > 8 ? 1 : 2) linear_rows_f3
 
 // How many CTAs split a block's contraction, and the time that it then takes beside what all have in common: what a cluster costs, and a
 // part for each step in the longest chain of them (one at least), which is longer where an SM has two CTAs.  In nanoseconds, fitted for
-// each kernel (RowsCost) to blocks of 48 matrices between 320 x 200 and 10240 x 5120 split by 1 to 8, with the weights in L2 and in DRAM: the
-// split it names takes 1.01 to 1.03 times as long as the best in the mean, 1.21 at most.  More CTAs than the device has places for (two per
-// SM, fewer for clusters: 33 of eight) are what costs most, 3.5 us for 2 x 5120 x 320 in clusters of four
-// (counted as 7, which keeps 2 x 10240 x 5120 in bf16 out of it, 22 us in one round and 24 from DRAM in two, and leaves it to fp32, 39 and
-// 37); powers of two up to two
-// CTAs per SM, the rule before, had 2 x 5120 x 1280 take 7.0 us, now 4.8, and 2 x 5120 x 640 5.4, now 3.7.
+// each kernel (RowsCost) to blocks of 48 matrices between 320 x 200 and 10240 x 5120 split by 1 to 8, with the weights in L2 and in DRAM:
+// the split it names takes 1.01 to 1.03 times as long as the best in the mean, 1.21 at most.  What costs most is more CTAs than the
+// device has places for (two per SM, fewer for clusters: 33 of eight): a second round of clusters took 3.5 us more for 2 x 5120 x 320 split by
+// four.  It is counted as 7, which leaves 2 x 10240 x 5120 in bf16 unsplit (22 us; 24 from DRAM in two rounds) and splits it in fp32 (39 unsplit,
+// 37).  Powers of two up to two CTAs per SM, the rule before, had 2 x 5120 x 1280 take 7.0 us, now 4.8, and 2 x 5120 x 640 5.4, now 3.7.
 struct RowsCost {
   int cluster, one, two, both, chains;  // ..., a step with one CTA on an SM, with two, what two have besides, chains of steps in a CTA
 };

@@ -50,8 +50,14 @@ __device__ __forceinline__ float max_row(float v, float* red, int t) {
 
 // Blocks of an SM at once: as many as the registers of a thread allow.  It holds kVec packets of x, delta and weight as they lie in memory
 // and of h as floats, and some 30 besides; 64 registers make four blocks of 256 threads, 84 three, 128 two.
+template <typename T, bool kAdd, int kVec>
+constexpr int kNormRegs = kVec * (8 + (int)sizeof(T) * (kAdd ? 6 : 4)) + 30;
 template <typename T, bool kAdd, int kLanes, int kVec>
-constexpr int kNormCtas = kLanes > 256 ? (kVec * sizeof(T) <= 4 ? 2 : 1) : kVec * (sizeof(T) == 2 ? (kAdd ? 20 : 16) : (kAdd ? 32 : 24)) + 30 <= 64 ? 4 : kVec * (sizeof(T) == 2 ? (kAdd ? 20 : 16) : (kAdd ? 32 : 24)) + 30 <= 84 ? 3 : kVec * (sizeof(T) == 2 ? (kAdd ? 20 : 16) : (kAdd ? 32 : 24)) + 30 <= 128 ? 2 : 1;
+constexpr int kNormCtas = kLanes > 256 ? (kVec * sizeof(T) <= 4 ? 2 : 1)  // (of 512 threads)
+                          : kNormRegs<T, kAdd, kVec> <= 64  ? 4
+                          : kNormRegs<T, kAdd, kVec> <= 84  ? 3
+                          : kNormRegs<T, kAdd, kVec> <= 128 ? 2
+                                                            : 1;
 
 // Packets of eight elements as they lie in memory.
 template <typename T> struct Raw;
