@@ -1,4 +1,5 @@
 // Test-only entry points.  toma_test_linear_form: the projections' rule of tile forms for any device, without one.
+// toma_test_linear_plus_form: the form that a projection with its epilogue takes on the current device.
 // toma_test_wait_timeout: makes a bounded device-side wait run out, the way every wait in the
 // tensor-core kernels would if its producer never came, and shows that the kernel then reports
 // through the status word and returns instead of hanging.
@@ -40,6 +41,6 @@ extern "C" toma_status toma_test_wait_timeout(uint32_t polls, uint32_t* dev_stat
 }
 
 extern "C" int32_t toma_test_linear_plus_form(int32_t m, int32_t n, int32_t k, int32_t e4m3, int32_t act) {
-  if (!toma::linear_tc_shape_ok(m, n, k) || act < TOMA_ACT_NONE || act > TOMA_ACT_SILU) return 0;
+  if (!toma::linear_tc_shape_ok(m, n, k) || m > 1 << 30 || n > 1 << 24 || k > 1 << 24 || act < TOMA_ACT_NONE || act > TOMA_ACT_SILU) return 0;
   return toma::linear_plus_form(m, n, k, e4m3 != 0, act);
 }

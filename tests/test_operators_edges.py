@@ -306,6 +306,7 @@ def test_forms_by_themselves(toma, tuning):  # noqa: F811
 def test_forms_of_bad_shapes(toma):  # noqa: F811
     form = toma.lib.toma_test_linear_plus_form
     assert form(0, 8, 8, 0, 0) == 0 and form(8, 12, 8, 0, 0) == 0 and form(8, 8, 8, 0, 4) == 0
+    assert form(2 ** 31 - 1, 8, 8, 0, 0) == 0 and form(8, 2 ** 31 - 8, 8, 0, 0) == 0 and form(8, 8, 2 ** 31 - 8, 1, 0) == 0
 
 
 # ---- fp32 on the tensor cores: none of the six products missing, chains as short as they are ----
